@@ -390,6 +390,52 @@ int32_t lpm_layerwise_backward(lpm_layerwise* lw, const void* x, const void* dz,
 int32_t lpm_layerwise_time(lpm_layerwise* lw, int32_t op, const void* x, const void* w, const void* wt, void* y, void* dx,
                            float* dw, void* ws, int32_t warmup, int32_t iters, void* stream, float* avg_us);
 
+/* ---- single operators of a pre-norm attention block ------------------------------------------------
+ * Beside the layers of a stage, as lpm_conv_* are: calls on caller-owned buffers that only enqueue. */
+
+/* Activation checkpoints in 8 bits: half (a quarter) of the bytes that a stash slot spends on a tensor between F and B.
+ * A tensor is [rows][channels].  Blocks of 32 consecutive channels of a row (the last one of a row may be shorter) share a power of two: k
+ * is the least integer >= -126 with max|x| 2^-k <= 127, an element becomes q = rint(x 2^-k) (int8, ties to even) and stands for
+ * q 2^k, which both element types hold exactly.  A block that holds an infinity or a NaN comes back as NaN.
+ * A checkpoint is one buffer of lpm_ckpt8_bytes: the q as [rows][channels], and from the next multiple of 256 bytes on the bytes
+ * k + 127 as [rows][ceil(channels / 32)] (255: NaN).  rows may be 0.
+ * Errors: LPM_EINVAL, LPM_ESHAPE (channels outside 1 .. 2^24, more than 2^40 elements), LPM_EALIGN, LPM_EHIP. */
+int32_t lpm_ckpt8_bytes(int64_t rows, int32_t channels, size_t* bytes);
+int32_t lpm_ckpt8_pack(int64_t rows, int32_t channels, int32_t dtype, const void* x, void* ckpt, void* stream);
+int32_t lpm_ckpt8_unpack(int64_t rows, int32_t channels, int32_t dtype, const void* ckpt, void* x, void* stream);
+
+/* lpm_conv_wgrad of a layer whose input was kept as a checkpoint (rows = the input's positions, channels = cin): the weight gradient
+ * for the values that the checkpoint stands for.  ws: lpm_conv_wgrad_ckpt8_ws_bytes.
+ * Errors: as lpm_conv_wgrad. */
+int32_t lpm_conv_wgrad_ckpt8_ws_bytes(const lpm_conv_geom* g, int32_t dtype, size_t* bytes);
+int32_t lpm_conv_wgrad_ckpt8(const lpm_conv_geom* g, int32_t dtype, const void* ckpt, const void* dz, float* dw, int32_t accumulate,
+                             void* ws, void* stream);
+
+/* Layer normalisation over the channels of every row: mu = mean x, r = 1 / sqrt(mean (x - mu)^2 + eps),
+ * y = gamma (x - mu) r + beta.  rows may be 0, channels 1 .. 16384.
+ *   x, y          [rows][channels]; y may be x
+ *   gamma, beta   float [channels], or NULL (1, 0)
+ *   stats         float [rows][2], mu and r for the backward pass; NULL = not wanted
+ *   ckpt          NULL, or a checkpoint of x, as lpm_ckpt8_pack writes it, stored in the same pass
+ * Errors: LPM_EINVAL, LPM_ESHAPE, LPM_EALIGN, LPM_EHIP. */
+int32_t lpm_norm_forward(int64_t rows, int32_t channels, int32_t dtype, const void* x, const float* gamma, const float* beta, float eps,
+                         void* y, float* stats, void* ckpt, void* stream);
+
+/* Scratch bytes of lpm_norm_backward. */
+int32_t lpm_norm_ws_bytes(int64_t rows, int32_t channels, int32_t dtype, size_t* bytes);
+
+/* The backward pass of lpm_norm_forward: with h = (x - mu) r and g = dy gamma,
+ * dx (+)= r (g - mean g - h mean(g h)), dgamma (+)= sum over rows of dy h, dbeta (+)= sum over rows of dy.
+ *   x or ckpt      the input, or its checkpoint: one of them, the other NULL
+ *   stats          as the forward pass left it
+ *   dx             dx_accumulate = 0 overwrites, 1 adds (a residual's gradient is already there); may be dy
+ *   dgamma, dbeta  float [channels], may be NULL; accumulate = 0 overwrites, 1 adds (gradient accumulation over micro-batches)
+ *   ws             lpm_norm_ws_bytes; may be NULL when neither gradient is wanted
+ * The order of every sum depends on the sizes alone.  Errors: as lpm_norm_forward. */
+int32_t lpm_norm_backward(int64_t rows, int32_t channels, int32_t dtype, const void* x, const void* ckpt, const float* stats, const void* dy,
+                          const float* gamma, void* dx, int32_t dx_accumulate, float* dgamma, float* dbeta, int32_t accumulate, void* ws,
+                          void* stream);
+
 #ifdef __cplusplus
 }
 #endif

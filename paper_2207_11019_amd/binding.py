@@ -9,7 +9,8 @@ import os
 
 import numpy as np
 
-__all__ = ["LpmError", "lib", "lpm_conv_geom", "lpm_conv_ws_bytes", "lpm_conv_forward", "lpm_conv_dgrad", "lpm_conv_wgrad", "lpm_conv_wgrad_static", "STATIC_SCRATCH_BYTES", "lpm_conv_time", "Layerwise", "lpm_layer", "lpm_cost_params", "lpm_stage_buffers", "layers_from_dicts",
+__all__ = ["LpmError", "lib", "lpm_conv_geom", "lpm_conv_ws_bytes", "lpm_conv_forward", "lpm_conv_dgrad", "lpm_conv_wgrad", "lpm_conv_wgrad_static", "STATIC_SCRATCH_BYTES", "lpm_conv_time", "lpm_ckpt8_bytes", "lpm_ckpt8_pack", "lpm_ckpt8_unpack",
+           "lpm_conv_wgrad_ckpt8", "lpm_conv_wgrad_ckpt8_ws_bytes", "lpm_norm_forward", "lpm_norm_backward", "lpm_norm_ws_bytes", "Layerwise", "lpm_layer", "lpm_cost_params", "lpm_stage_buffers", "layers_from_dicts",
            "lpm_layer_cost", "lpm_partition", "lpm_partition_costs", "Stage", "Schedule", "Net", "F32", "BF16", "LOCKED", "OVERLAPPED", "PIPELINED", "ASYNC_UPDATE",
            "GRAPH", "pack_act", "unpack_act", "pack_weight", "unpack_weight", "MI355X_COST"]
 
@@ -91,7 +92,16 @@ lib.lpm_layerwise_ws_bytes.argtypes = [_vp, _psz, _psz]
 lib.lpm_layerwise_forward.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp]
 lib.lpm_layerwise_backward.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp]
 lib.lpm_layerwise_time.argtypes = [_vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _vp, C.POINTER(C.c_float)]
-for _f in ("lpm_layerwise_create", "lpm_layerwise_destroy", "lpm_layerwise_ws_bytes", "lpm_layerwise_forward",
+_i64, _f32 = C.c_int64, C.c_float
+lib.lpm_ckpt8_bytes.argtypes = [_i64, _i32, _psz]
+lib.lpm_ckpt8_pack.argtypes = lib.lpm_ckpt8_unpack.argtypes = [_i64, _i32, _i32, _vp, _vp, _vp]
+lib.lpm_conv_wgrad_ckpt8_ws_bytes.argtypes = [C.POINTER(lpm_conv_geom), _i32, _psz]
+lib.lpm_conv_wgrad_ckpt8.argtypes = [C.POINTER(lpm_conv_geom), _i32, _vp, _vp, _vp, _i32, _vp, _vp]
+lib.lpm_norm_ws_bytes.argtypes = [_i64, _i32, _i32, _psz]
+lib.lpm_norm_forward.argtypes = [_i64, _i32, _i32, _vp, _vp, _vp, _f32, _vp, _vp, _vp, _vp]
+lib.lpm_norm_backward.argtypes = [_i64, _i32, _i32] + [_vp] * 6 + [_i32, _vp, _vp, _i32, _vp, _vp]
+for _f in ("lpm_ckpt8_bytes", "lpm_ckpt8_pack", "lpm_ckpt8_unpack", "lpm_conv_wgrad_ckpt8", "lpm_conv_wgrad_ckpt8_ws_bytes", "lpm_norm_forward",
+           "lpm_norm_backward", "lpm_norm_ws_bytes", "lpm_layerwise_create", "lpm_layerwise_destroy", "lpm_layerwise_ws_bytes", "lpm_layerwise_forward",
            "lpm_layerwise_backward", "lpm_layerwise_time", "lpm_conv_time", "lpm_conv_ws_bytes", "lpm_conv_forward", "lpm_conv_dgrad", "lpm_conv_wgrad", "lpm_conv_wgrad_static", "lpm_layer_cost", "lpm_partition", "lpm_partition_costs", "lpm_stage_create", "lpm_stage_destroy", "lpm_stage_sizes",
            "lpm_stage_param_offset", "lpm_stage_stash_offset", "lpm_stage_grad_offset", "lpm_stage_sync_lowp",
            "lpm_stage_forward", "lpm_stage_backward", "lpm_stage_update", "lpm_schedule_create",
@@ -250,6 +260,102 @@ def lpm_conv_time(op, g, dtype, x, w, wt, y, dw, ws, warmup=3, iters=20, stream=
     _check(lib.lpm_conv_time(op, C.byref(gg), dtype, _ptr(x), _ptr(w), _ptr(wt), _ptr(y), _ptr(dw), _ptr(ws), warmup, iters,
                              _stream(stream), C.byref(out)))
     return out.value
+
+
+def _elem(dtype):
+    return 2 if dtype == BF16 else 4
+
+
+_NAMES = {F32: "torch.float32", BF16: "torch.bfloat16"}
+
+
+def _takes(name, t, nbytes, kind=None):
+    """_holds, and for the operators whose operands are tensors of one element type: that type (or bytes), dense, on the current GPU."""
+    if t is None or isinstance(t, int):
+        return
+    if kind is not None and str(t.dtype) not in (kind, "torch.uint8"):
+        raise ValueError("%s is a tensor of %s, the call takes %s" % (name, t.dtype, kind))
+    if not t.is_contiguous():
+        raise ValueError("%s is not dense" % name)
+    _on_this_gpu(name, t)
+    _holds(name, t, nbytes)
+
+
+def _on_this_gpu(name, t):
+    if t.is_cuda:
+        import torch
+        if t.device.index != torch.cuda.current_device():
+            raise ValueError("%s is on %s, the current device is %d" % (name, t.device, torch.cuda.current_device()))
+
+
+def lpm_ckpt8_bytes(rows, channels):
+    """Bytes of the 8-bit checkpoint of a tensor [rows][channels]."""
+    n = C.c_size_t()
+    _check(lib.lpm_ckpt8_bytes(rows, channels, C.byref(n)))
+    return n.value
+
+
+def lpm_ckpt8_pack(rows, channels, dtype, x, ckpt, stream=None):
+    """ckpt = the 8-bit checkpoint of x."""
+    kept = lpm_ckpt8_bytes(rows, channels)
+    _takes("x", x, rows * channels * _elem(dtype), _NAMES.get(dtype)), _takes("ckpt", ckpt, kept)
+    _check(lib.lpm_ckpt8_pack(rows, channels, dtype, _ptr(x), _ptr(ckpt), _stream(stream)))
+
+
+def lpm_ckpt8_unpack(rows, channels, dtype, ckpt, x, stream=None):
+    """x = the values that ckpt stands for."""
+    kept = lpm_ckpt8_bytes(rows, channels)
+    _takes("x", x, rows * channels * _elem(dtype), _NAMES.get(dtype)), _takes("ckpt", ckpt, kept)
+    _check(lib.lpm_ckpt8_unpack(rows, channels, dtype, _ptr(ckpt), _ptr(x), _stream(stream)))
+
+
+def lpm_conv_wgrad_ckpt8_ws_bytes(g, dtype):
+    gg, n = _geom(g), C.c_size_t()
+    _check(lib.lpm_conv_wgrad_ckpt8_ws_bytes(C.byref(gg), dtype, C.byref(n)))
+    return n.value
+
+
+def lpm_conv_wgrad_ckpt8(g, dtype, ckpt, dz, dw, accumulate=False, ws=None, stream=None):
+    """lpm_conv_wgrad for the input that ckpt stands for."""
+    gg = _geom(g)
+    need = lpm_conv_wgrad_ckpt8_ws_bytes(gg, dtype)
+    _, yb, _, db = _conv_sizes(gg, dtype)
+    _takes("ckpt", ckpt, lpm_ckpt8_bytes(gg.m * max(gg.d, 1) * gg.h * gg.w, gg.cin)), _takes("dz", dz, yb, _NAMES.get(dtype))
+    _takes("dw", dw, db, _NAMES[F32]), _takes("ws", ws, need)
+    _check(lib.lpm_conv_wgrad_ckpt8(C.byref(gg), dtype, _ptr(ckpt), _ptr(dz), _ptr(dw), int(accumulate), _ptr(ws), _stream(stream)))
+
+
+def lpm_norm_ws_bytes(rows, channels, dtype):
+    """Scratch bytes of lpm_norm_backward."""
+    n = C.c_size_t()
+    _check(lib.lpm_norm_ws_bytes(rows, channels, dtype, C.byref(n)))
+    return n.value
+
+
+def _norm_holds(rows, channels, dtype, full, line, stats, ckpt):
+    lpm_norm_ws_bytes(rows, channels, dtype)      # (refuses a bad shape before sizes are worked out from it)
+    for name, t in full.items():
+        _takes(name, t, rows * channels * _elem(dtype), _NAMES[dtype])
+    for name, t in line.items():
+        _takes(name, t, channels * 4, _NAMES[F32])
+    _takes("stats", stats, rows * 8, _NAMES[F32])
+    if ckpt is not None:
+        _takes("ckpt", ckpt, lpm_ckpt8_bytes(rows, channels))
+
+
+def lpm_norm_forward(rows, channels, dtype, x, gamma, beta, eps, y, stats=None, ckpt=None, stream=None):
+    """Layer norm of [rows][channels]; stats and ckpt (the input's 8-bit checkpoint) are what the backward pass may ask for."""
+    _norm_holds(rows, channels, dtype, dict(x=x, y=y), dict(gamma=gamma, beta=beta), stats, ckpt)
+    _check(lib.lpm_norm_forward(rows, channels, dtype, _ptr(x), _ptr(gamma), _ptr(beta), eps, _ptr(y), _ptr(stats), _ptr(ckpt), _stream(stream)))
+
+
+def lpm_norm_backward(rows, channels, dtype, x, ckpt, stats, dy, gamma, dx, dgamma=None, dbeta=None, dx_accumulate=False, accumulate=False, ws=None,
+                      stream=None):
+    """Gradients of lpm_norm_forward from the input x or its checkpoint (the other one None)."""
+    _norm_holds(rows, channels, dtype, dict(x=x, dy=dy, dx=dx), dict(gamma=gamma, dgamma=dgamma, dbeta=dbeta), stats, ckpt)
+    _takes("ws", ws, lpm_norm_ws_bytes(rows, channels, dtype))
+    _check(lib.lpm_norm_backward(rows, channels, dtype, _ptr(x), _ptr(ckpt), _ptr(stats), _ptr(dy), _ptr(gamma), _ptr(dx), int(dx_accumulate),
+                                 _ptr(dgamma), _ptr(dbeta), int(accumulate), _ptr(ws), _stream(stream)))
 
 
 class Layerwise:

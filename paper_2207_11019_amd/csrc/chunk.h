@@ -1,0 +1,84 @@
+// Eight consecutive channels of a row, and the 8-bit form in which a checkpoint keeps them.
+#pragma once
+#include "elem.h"
+#include <cstring>
+
+namespace lpm {
+
+// Rows of any channel count start anywhere: the accesses are 16 (8) bytes wide and aligned to an element only, which global memory takes.
+__device__ __forceinline__ void ld_chunk(const float* p, float (&v)[8]) { __builtin_memcpy(v, p, 32); }
+__device__ __forceinline__ void ld_chunk(const bf16_t* p, float (&v)[8]) {
+    uint32_t w[4];
+    __builtin_memcpy(w, p, 16);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(w[e] << 16); v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u); }
+}
+__device__ __forceinline__ void st_chunk(float* p, const float (&v)[8]) { __builtin_memcpy(p, v, 32); }
+__device__ __forceinline__ void st_chunk(bf16_t* p, const float (&v)[8]) {
+    const uint32_t w[4] = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    __builtin_memcpy(p, w, 16);
+}
+// ... the first n of them, 0 beyond (n may be negative or more than eight)
+template <typename T> __device__ __forceinline__ void ld_chunk(const T* p, int n, float (&v)[8]) {
+    if (n >= 8) { ld_chunk(p, v); return; }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? ld(p, e) : 0.f;
+}
+template <typename T> __device__ __forceinline__ void st_chunk(T* p, int n, const float (&v)[8]) {
+    if (n >= 8) { st_chunk(p, v); return; }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) if (e < n) st(p, e, v[e]);
+}
+
+// ---- checkpoints in 8 bits ----
+// A block is CKPT_BLOCK consecutive channels of a row (the last of a row may be shorter): k is the least integer >= -126 with
+// max|x| 2^-k <= 127, an element is q = rint(x 2^-k) in int8, ties to even, and stands for q 2^k.  A power of two and eight bits: scaling is exact, and so
+// is what comes back, in bfloat16 too -- the only rounding is that to a whole q, at most half a step of 1/127 to 1/63.5 of the block's
+// largest element.  Kept are the q and the byte k + 127; byte 255: the block holds an infinity or a NaN and comes back as NaN.
+constexpr int CKPT_BLOCK = 32;
+constexpr uint32_t CKPT_BAD = 255;
+__device__ __forceinline__ float pow2(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }      // -126 <= k <= 127
+// the byte of a block whose largest magnitude has these bits
+__device__ __forceinline__ uint32_t ckpt_byte(uint32_t top) {
+    if (top >= 0x7f800000u) return CKPT_BAD;
+    const int k = (int)(top >> 23) - 127 - ((top & 0x7fffffu) <= 0x7e0000u ? 6 : 5);      // 127 = 1.984375 * 2^6
+    return (uint32_t)((k < -126 ? -126 : k) + 127);
+}
+__device__ __forceinline__ uint32_t chunk_top(const float (&v)[8]) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { const uint32_t a = __float_as_uint(v[e]) & 0x7fffffffu; m = a > m ? a : m; }
+    return m;
+}
+// eight elements as bytes; of a bad block, zeros
+__device__ __forceinline__ uint2 ckpt_quantise(const float (&v)[8], uint32_t byte) {
+    const float up = pow2(byte == CKPT_BAD ? 0 : 127 - (int)byte);
+    uint32_t w[2] = {0, 0};
+    if (byte != CKPT_BAD) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e >> 2] |= ((uint32_t)(int)rintf(v[e] * up) & 0xffu) << (8 * (e & 3));
+    }
+    return make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ void ckpt_values(uint2 q, uint32_t byte, float (&v)[8]) {
+    const float step = byte == CKPT_BAD ? __uint_as_float(0x7fc00000u) : pow2((int)byte - 127);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)(int8_t)((e < 4 ? q.x : q.y) >> (8 * (e & 3))) * step;
+}
+__device__ __forceinline__ uint2 ld_bytes8(const uint8_t* p, int n) {
+    uint2 q = make_uint2(0, 0);
+    if (n >= 8) { __builtin_memcpy(&q, p, 8); return q; }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) if (e < n) (e < 4 ? q.x : q.y) |= (uint32_t)p[e] << (8 * (e & 3));
+    return q;
+}
+__device__ __forceinline__ void st_bytes8(uint8_t* p, int n, uint2 q) {
+    if (n >= 8) { __builtin_memcpy(p, &q, 8); return; }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) if (e < n) p[e] = (uint8_t)((e < 4 ? q.x : q.y) >> (8 * (e & 3)));
+}
+// where the bytes k + 127 of a checkpoint lie: behind the rows' q, on a 256-byte boundary, ckpt_blocks(channels) to a row
+__host__ __device__ inline int ckpt_blocks(int channels) { return (channels + CKPT_BLOCK - 1) / CKPT_BLOCK; }
+__host__ __device__ inline size_t ckpt_exponents_at(int64_t rows, int channels) { return ((size_t)rows * channels + 255) & ~(size_t)255; }
+
+}  // namespace lpm

@@ -240,6 +240,9 @@ hipError_t launch_f32_to_bf16(const float* src, uint16_t* dst, size_t n, hipStre
 struct TransposeDesc { const float* src; uint16_t* dst; int32_t Cout, KK, Cin; const float* scale; };
 constexpr int LPM_TRANSPOSE_BATCH = 24;
 hipError_t launch_weight_transpose_batch(const TransposeDesc* d, int count, hipStream_t st);
+// checkpoints in 8 bits of [rows][C]: q, and from the next multiple of 256 bytes on the blocks' exponents
+hipError_t launch_ckpt8_pack(int dtype, int64_t rows, int32_t C, const void* x, void* ckpt, hipStream_t st);
+hipError_t launch_ckpt8_unpack(int dtype, int64_t rows, int32_t C, const void* ckpt, void* x, hipStream_t st);
 hipError_t launch_fill_f32(float* p, size_t n, float v, hipStream_t st);
 
 }  // namespace lpm
