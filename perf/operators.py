@@ -196,7 +196,7 @@ def _buffers(s):
         fwd, bwd = lpm.lpm_attn_ws_bytes(s["g"], dt)
         s["y"] = torch.empty(c["m"], c["pq"], c["heads"] * c["d"], dtype=_tdt(c), device="cuda")
         s["ws"] = buf(max(fwd, bwd if c["train"] else 0))
-        s["stats"] = torch.empty(c["m"] * c["heads"] * c["pq"] * 2, device="cuda") if c["train"] else None
+        s["stats"] = buf(lpm.lpm_attn_stats_bytes(s["g"], dt)) if c["train"] else None
         if c["train"]:
             H = c["heads"] * c["d"]
             if c["packed"]:
