@@ -436,6 +436,48 @@ int32_t lpm_norm_backward(int64_t rows, int32_t channels, int32_t dtype, const v
                           const float* gamma, void* dx, int32_t dx_accumulate, float* dgamma, float* dbeta, int32_t accumulate, void* ws,
                           void* stream);
 
+/* Multi-head attention with a learned bias by the bucket of the distance between key and query:
+ *   s_ij = scale q_i.k_j + table[h][map[clamp(j - (i + q_start[n]), -reach, reach) + reach]],   y_i = sum_j softmax_j(s_ij) v_j
+ * over the visible keys of sample n: j < key_len[n], and j <= i + q_start[n] when causal.  A query without visible keys, or with scores of
+ * -infinity alone, gives zeros and has no gradients.
+ *   q, y     [m][pq][heads][d], positions ldq, ldy elements apart        k, v   [m][pk][kv_heads][d], positions ldk, ldv apart
+ *            (0: dense).  Query head h reads key and value head h / (heads / kv_heads).  A packed tensor queries | keys | values, as
+ *            LPM_ATTN takes it, is three pointers into it and ldq = ldk = ldv = 3 * heads * d.  q, k, v and their gradients need the alignment
+ *            of an element only.
+ *   key_len  int32 [m], keys of a sample (clamped to 0 .. pk), NULL: pk.  Keys and values behind it are not read.  Values of keys that causal alone
+ *            hides from some queries have to be finite.
+ *   q_start  int32 [m], position of a sample's query 0 among its keys: 0 in self-attention, key_len - pq where the queries are the youngest
+ *            positions of a cache; NULL: 0
+ *   map      int32 [2 * reach + 1], the bucket (clamped to 0 .. n_buckets - 1) of every distance key - query from -reach to reach; distances beyond
+ *            have the bucket of the end.  lpm_relbias_buckets makes the usual one.
+ *   table    float [heads][n_buckets]; n_buckets = 0, map = table = NULL: no bias
+ *   scale    0: 1 / sqrt(d)
+ * Limits: d 1 .. 128, heads up to 65535, reach up to 2048, n_buckets up to 65536, pq and pk 0 .. 2^28. */
+typedef struct lpm_attn_geom {
+    int32_t m, heads, kv_heads, pq, pk, d, causal, n_buckets, reach, ldq, ldk, ldv, ldy;
+    float scale;
+} lpm_attn_geom;
+
+/* Scratch of the two passes, and what the forward pass keeps for the backward pass beside q, k, v and y (host out-pointers). */
+int32_t lpm_attn_ws_bytes(const lpm_attn_geom* g, int32_t dtype, size_t* forward, size_t* backward);
+int32_t lpm_attn_stats_bytes(const lpm_attn_geom* g, int32_t dtype, size_t* bytes);
+
+/* stats: NULL when there will be no backward pass.  Errors: LPM_EINVAL, LPM_ESHAPE, LPM_EALIGN, LPM_EHIP. */
+int32_t lpm_attn_forward(const lpm_attn_geom* g, int32_t dtype, const void* q, const void* k, const void* v, const int32_t* key_len,
+                         const int32_t* q_start, const int32_t* map, const float* table, void* y, void* stats, void* ws, void* stream);
+
+/* dq, dk, dv (laid out and spaced like q, k, v; written, keys behind key_len with zeros) and dtable (float, (+)=: accumulate = 0 overwrites, 1 adds;
+ * NULL: not wanted) from dy (spaced like y) and what the forward pass read and left.  The order of every sum depends on the sizes and key_len
+ * alone.  Errors: as lpm_attn_forward. */
+int32_t lpm_attn_backward(const lpm_attn_geom* g, int32_t dtype, const void* q, const void* k, const void* v, const void* y, const void* stats,
+                          const void* dy, const int32_t* key_len, const int32_t* q_start, const int32_t* map, const float* table, void* dq,
+                          void* dk, void* dv, float* dtable, int32_t accumulate, void* ws, void* stream);
+
+/* The usual map of distances to buckets (map: host, 2 * reach + 1 entries): half of a side's buckets for the nearest distances, one each, the rest
+ * by the logarithm up to reach.  both_sides != 0: keys before and behind the query have half of the (even) n_buckets each, behind from
+ * n_buckets / 2 on; 0: keys behind the query share bucket 0 with the query's own position.  Errors: LPM_EINVAL. */
+int32_t lpm_relbias_buckets(int32_t n_buckets, int32_t reach, int32_t both_sides, int32_t* map);
+
 #ifdef __cplusplus
 }
 #endif

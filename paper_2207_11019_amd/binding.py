@@ -10,7 +10,8 @@ import os
 import numpy as np
 
 __all__ = ["LpmError", "lib", "lpm_conv_geom", "lpm_conv_ws_bytes", "lpm_conv_forward", "lpm_conv_dgrad", "lpm_conv_wgrad", "lpm_conv_wgrad_static", "STATIC_SCRATCH_BYTES", "lpm_conv_time", "lpm_ckpt8_bytes", "lpm_ckpt8_pack", "lpm_ckpt8_unpack",
-           "lpm_conv_wgrad_ckpt8", "lpm_conv_wgrad_ckpt8_ws_bytes", "lpm_norm_forward", "lpm_norm_backward", "lpm_norm_ws_bytes", "Layerwise", "lpm_layer", "lpm_cost_params", "lpm_stage_buffers", "layers_from_dicts",
+           "lpm_conv_wgrad_ckpt8", "lpm_conv_wgrad_ckpt8_ws_bytes", "lpm_norm_forward", "lpm_norm_backward", "lpm_norm_ws_bytes",
+           "lpm_attn_geom", "lpm_attn_ws_bytes", "lpm_attn_stats_bytes", "lpm_attn_forward", "lpm_attn_backward", "lpm_relbias_buckets", "Layerwise", "lpm_layer", "lpm_cost_params", "lpm_stage_buffers", "layers_from_dicts",
            "lpm_layer_cost", "lpm_partition", "lpm_partition_costs", "Stage", "Schedule", "Net", "F32", "BF16", "LOCKED", "OVERLAPPED", "PIPELINED", "ASYNC_UPDATE",
            "GRAPH", "pack_act", "unpack_act", "pack_weight", "unpack_weight", "MI355X_COST"]
 
@@ -52,6 +53,11 @@ class lpm_stage_buffers(C.Structure):
 
 class lpm_conv_geom(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("m", "h", "w", "cin", "cout", "kh", "kw", "stride", "pad", "d", "kd", "pad_d")]
+
+
+class lpm_attn_geom(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("m", "heads", "kv_heads", "pq", "pk", "d", "causal", "n_buckets", "reach", "ldq", "ldk", "ldv", "ldy")] + \
+               [("scale", C.c_float)]
 
 
 lib.lpm_last_error.restype = C.c_char_p
@@ -100,7 +106,13 @@ lib.lpm_conv_wgrad_ckpt8.argtypes = [C.POINTER(lpm_conv_geom), _i32, _vp, _vp, _
 lib.lpm_norm_ws_bytes.argtypes = [_i64, _i32, _i32, _psz]
 lib.lpm_norm_forward.argtypes = [_i64, _i32, _i32, _vp, _vp, _vp, _f32, _vp, _vp, _vp, _vp]
 lib.lpm_norm_backward.argtypes = [_i64, _i32, _i32] + [_vp] * 6 + [_i32, _vp, _vp, _i32, _vp, _vp]
-for _f in ("lpm_ckpt8_bytes", "lpm_ckpt8_pack", "lpm_ckpt8_unpack", "lpm_conv_wgrad_ckpt8", "lpm_conv_wgrad_ckpt8_ws_bytes", "lpm_norm_forward",
+_pag = C.POINTER(lpm_attn_geom)
+lib.lpm_attn_ws_bytes.argtypes = [_pag, _i32, _psz, _psz]
+lib.lpm_attn_stats_bytes.argtypes = [_pag, _i32, _psz]
+lib.lpm_attn_forward.argtypes = [_pag, _i32] + [_vp] * 11
+lib.lpm_attn_backward.argtypes = [_pag, _i32] + [_vp] * 14 + [_i32, _vp, _vp]
+lib.lpm_relbias_buckets.argtypes = [_i32, _i32, _i32, C.POINTER(_i32)]
+for _f in ("lpm_attn_ws_bytes", "lpm_attn_stats_bytes", "lpm_attn_forward", "lpm_attn_backward", "lpm_relbias_buckets", "lpm_ckpt8_bytes", "lpm_ckpt8_pack", "lpm_ckpt8_unpack", "lpm_conv_wgrad_ckpt8", "lpm_conv_wgrad_ckpt8_ws_bytes", "lpm_norm_forward",
            "lpm_norm_backward", "lpm_norm_ws_bytes", "lpm_layerwise_create", "lpm_layerwise_destroy", "lpm_layerwise_ws_bytes", "lpm_layerwise_forward",
            "lpm_layerwise_backward", "lpm_layerwise_time", "lpm_conv_time", "lpm_conv_ws_bytes", "lpm_conv_forward", "lpm_conv_dgrad", "lpm_conv_wgrad", "lpm_conv_wgrad_static", "lpm_layer_cost", "lpm_partition", "lpm_partition_costs", "lpm_stage_create", "lpm_stage_destroy", "lpm_stage_sizes",
            "lpm_stage_param_offset", "lpm_stage_stash_offset", "lpm_stage_grad_offset", "lpm_stage_sync_lowp",
@@ -356,6 +368,79 @@ def lpm_norm_backward(rows, channels, dtype, x, ckpt, stats, dy, gamma, dx, dgam
     _takes("ws", ws, lpm_norm_ws_bytes(rows, channels, dtype))
     _check(lib.lpm_norm_backward(rows, channels, dtype, _ptr(x), _ptr(ckpt), _ptr(stats), _ptr(dy), _ptr(gamma), _ptr(dx), int(dx_accumulate),
                                  _ptr(dgamma), _ptr(dbeta), int(accumulate), _ptr(ws), _stream(stream)))
+
+
+def _attn_geom(g):
+    return g if isinstance(g, lpm_attn_geom) else lpm_attn_geom(**g)
+
+
+def lpm_attn_ws_bytes(g, dtype):
+    """-> (forward, backward) scratch bytes"""
+    f, b, gg = C.c_size_t(), C.c_size_t(), _attn_geom(g)
+    _check(lib.lpm_attn_ws_bytes(C.byref(gg), dtype, C.byref(f), C.byref(b)))
+    return f.value, b.value
+
+
+def lpm_attn_stats_bytes(g, dtype):
+    """Bytes of what the forward pass keeps for the backward pass beside its operands and result."""
+    n, gg = C.c_size_t(), _attn_geom(g)
+    _check(lib.lpm_attn_stats_bytes(C.byref(gg), dtype, C.byref(n)))
+    return n.value
+
+
+def _spaced(name, t, dtype, positions, ld, width):
+    """The operand's positions, `ld` elements apart from its first element on, lie inside the tensor's memory: it may be a part of a packed tensor."""
+    if t is None or isinstance(t, int) or positions == 0:
+        return
+    if str(t.dtype) != _NAMES[dtype]:
+        raise ValueError("%s is a tensor of %s, the call takes %s" % (name, t.dtype, _NAMES[dtype]))
+    if t.dim() > 0 and t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError("%s: the channels of a position do not lie side by side" % name)
+    _on_this_gpu(name, t)
+    have = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+    need = (positions - 1) * (ld or width) + width
+    if have < need:
+        raise ValueError("%s reaches over %d elements, the geometry needs %d" % (name, have, need))
+
+
+def _attn_holds(g, dtype, spaced, samples, bias, stats):
+    lpm_attn_ws_bytes(g, dtype)                   # (refuses a bad shape before sizes are worked out from it)
+    wq, wk = g.heads * g.d, g.kv_heads * g.d
+    for name, t in spaced.items():
+        kv = name.lstrip("d") in ("k", "v")
+        _spaced(name, t, dtype, g.m * (g.pk if kv else g.pq), getattr(g, "ld" + name.lstrip("d")), wk if kv else wq)
+    for name, t in samples.items():
+        _takes(name, t, 4 * g.m, "torch.int32")
+    _takes("map", bias[0], 4 * (2 * g.reach + 1), "torch.int32")
+    for t in bias[1:]:
+        _takes("table", t, 4 * g.heads * g.n_buckets, _NAMES[F32])
+    if stats is not None:
+        _takes("stats", stats, lpm_attn_stats_bytes(g, dtype))
+
+
+def lpm_attn_forward(g, dtype, q, k, v, key_len, q_start, map, table, y, stats=None, ws=None, stream=None):
+    """Attention with the bias table[h][map[distance]]; g: an lpm_attn_geom or its fields as a dict."""
+    gg = _attn_geom(g)
+    _attn_holds(gg, dtype, dict(q=q, k=k, v=v, y=y), dict(key_len=key_len, q_start=q_start), (map, table), stats)
+    _takes("ws", ws, lpm_attn_ws_bytes(gg, dtype)[0])
+    _check(lib.lpm_attn_forward(C.byref(gg), dtype, _ptr(q), _ptr(k), _ptr(v), _ptr(key_len), _ptr(q_start), _ptr(map), _ptr(table), _ptr(y), _ptr(stats),
+                                _ptr(ws), _stream(stream)))
+
+
+def lpm_attn_backward(g, dtype, q, k, v, y, stats, dy, key_len, q_start, map, table, dq, dk, dv, dtable=None, accumulate=False, ws=None, stream=None):
+    """Gradients of lpm_attn_forward; accumulate concerns dtable."""
+    gg = _attn_geom(g)
+    _attn_holds(gg, dtype, dict(q=q, k=k, v=v, y=y, dy=dy, dq=dq, dk=dk, dv=dv), dict(key_len=key_len, q_start=q_start), (map, table, dtable), stats)
+    _takes("ws", ws, lpm_attn_ws_bytes(gg, dtype)[1])
+    _check(lib.lpm_attn_backward(C.byref(gg), dtype, _ptr(q), _ptr(k), _ptr(v), _ptr(y), _ptr(stats), _ptr(dy), _ptr(key_len), _ptr(q_start), _ptr(map),
+                                 _ptr(table), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dtable), int(accumulate), _ptr(ws), _stream(stream)))
+
+
+def lpm_relbias_buckets(n_buckets, reach, both_sides=True):
+    """The usual map of distances -reach .. reach to buckets (list of 2 * reach + 1)."""
+    out = (C.c_int32 * (2 * max(reach, 0) + 1))()
+    _check(lib.lpm_relbias_buckets(n_buckets, reach, int(both_sides), out))
+    return list(out)
 
 
 class Layerwise:

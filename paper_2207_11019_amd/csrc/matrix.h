@@ -1,0 +1,89 @@
+// Operands of the 32x32 matrix instructions as 16-byte chunks: eight bfloat16 or four floats of a row.
+#pragma once
+#include "elem.h"
+#include <cstring>
+
+namespace lpm {
+
+typedef float mm_f16 __attribute__((ext_vector_type(16)));
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 mm_bf8;
+typedef unsigned int mm_u2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short mm_s4;
+
+// What a lane holds: of both operands, row (column) lane % 32 and of every 2 * EPC terms of the sum the EPC that belong to its half lane / 32;
+// of the result, column lane % 32 and rows (r & 3) + 8 (r >> 2) + 4 (lane / 32), r = 0 .. 15.
+template <typename T> struct Mm;
+template <> struct Mm<bf16_t> {
+    static constexpr int EPC = 8;
+    static __device__ __forceinline__ mm_f16 mul(uint4 a, uint4 b, mm_f16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(mm_bf8, a), __builtin_bit_cast(mm_bf8, b), c, 0, 0, 0);
+    }
+    // EPC values of the result as an operand of the next product
+    static __device__ __forceinline__ uint4 pack(const float* v) {
+        return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+    }
+    // The LDS transpose read: lane i of 16 receives element i % 4 of the four-element pieces that lanes 4j + i/4 point at, j = 0 .. 3.
+    static __device__ __forceinline__ uint2 read4(const unsigned char* p) {
+#ifdef __HIP__
+        return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) mm_s4*)(p)));
+#else       // the same by lane exchanges
+        unsigned e[4];
+        const int lane = threadIdx.x & 63;
+        for (int j = 0; j < 4; ++j) {
+            const unsigned char* q = __shfl(p, (lane & ~15) + 4 * j + (lane & 15) / 4, 64);
+            uint16_t w;
+            __builtin_memcpy(&w, q + 2 * (lane & 3), 2);
+            e[j] = w;
+        }
+        (void)__shfl(0, 0, 64);
+        return make_uint2(e[0] | e[1] << 16, e[2] | e[3] << 16);
+#endif
+    }
+    // operand whose rows are the columns col .. col + 31 of a tile in LDS and whose terms are its rows, in the order in which a result lies over
+    // the lanes: those of half g are row + 4 g + (0 .. 3) and row + 8 + 4 g + (0 .. 3)
+    static __device__ __forceinline__ uint4 columns(const unsigned char* tile, int pitch, int row, int col, int lane) {
+        const unsigned char* p = tile + (row + 4 * (lane >> 5) + ((lane >> 2) & 3)) * pitch + (col + (lane & 16) + 4 * (lane & 3)) * 2;
+        const uint2 a = read4(p), b = read4(p + 8 * pitch);
+        return make_uint4(a.x, a.y, b.x, b.y);
+    }
+};
+template <> struct Mm<float> {
+    static constexpr int EPC = 4;
+    static __device__ __forceinline__ mm_f16 mul(uint4 a, uint4 b, mm_f16 c) {
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint4 pack(const float* v) {
+        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    }
+    // ... the rows of half g: row + 4 g + (0 .. 3)
+    static __device__ __forceinline__ uint4 columns(const unsigned char* tile, int pitch, int row, int col, int lane) {
+        const unsigned char* p = tile + (row + 4 * (lane >> 5)) * pitch + (col + (lane & 31)) * 4;
+        return make_uint4(*(const unsigned*)p, *(const unsigned*)(p + pitch), *(const unsigned*)(p + 2 * pitch), *(const unsigned*)(p + 3 * pitch));
+    }
+};
+
+// 2^x for x <= 0 or so: one instruction (a result below 2^-126 is 0)
+__device__ __forceinline__ float exp2_fast(float x) {
+#ifdef __HIP_DEVICE_COMPILE__
+    return __builtin_amdgcn_exp2f(x);
+#else
+    return exp2f(x);
+#endif
+}
+
+// the first n of the EPC elements at p (an element's alignment is enough), zeros beyond; n may be negative or larger
+template <typename T> __device__ __forceinline__ uint4 ld16(const T* p, int n) {
+    constexpr int EPC = Mm<T>::EPC;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (n >= EPC) { __builtin_memcpy(&v, p, 16); return v; }
+    T e[EPC] = {};
+#pragma unroll
+    for (int k = 0; k < EPC; ++k) if (k < n) e[k] = p[k];
+    __builtin_memcpy(&v, e, 16);
+    return v;
+}
+
+}  // namespace lpm
