@@ -21,9 +21,10 @@ using namespace lpm;
 
 namespace lpm {
 
-constexpr int RA_THREADS = 256, RA_WAVES = 4, RA_BM = 128;
-constexpr int RA_PAD = 96;                // margin of the bias by distance: a tile that is not wholly beyond the reach stays within it (63 + 31)
+constexpr int RA_THREADS = 256, RA_WAVES = 4;
+constexpr int RA_PAD = 96;                // margin of the bias by distance: a tile of up to 64 x 32 that is not wholly beyond the reach stays within it
 constexpr int RA_MAX_REACH = 2048;
+constexpr int RA_MAX_LD = 1 << 23;         // elements between positions: 128 of them are offsets of 32 bits
 constexpr float RA_LOG2E = 1.4426950408889634f;
 constexpr int RA_DIAG_PITCH = 36;         // floats of a line of a wavefront's diagonals
 
@@ -31,40 +32,89 @@ struct float2_ { float x, y; };
 
 struct AttnArgs {
     int32_t m, H, G, pq, pk, d, causal, nb, reach, splits;
+    int32_t fold;                         // forward: a block's rows are the queries of all heads that share keys (few queries)
     int64_t ldq, ldk, ldv, ldy;           // elements between positions
     float scale, scale2;                  // scale2 = scale log2(e)
     const void *q, *k, *v, *dy;
     void *y, *dq, *dk, *dv;
     const int32_t *len, *start, *map;
     const float* table;
-    float2_* stats;                       // per row (n, h, i): maximum of the scores in units of log2, -log2 of the sum (-inf: no visible key)
-    bf16_t* low;                          // what the rounding of y took away, [m][pq][H d] (bfloat16)
+    float2_* stats;                       // per row (n, h, i): the softmax's reference in units of log2, and -log2 of the sum behind it (-inf: no visible key)
     float *part, *part_ml;                // splits: [split][row][d] and [split][row][2]
-    float *delta, *diag;                  // backward: [row], [m H ceil(pq / 32)][2 reach + 1]
+    float *delta, *diag;                  // backward: [row], [m H][lines][2 reach + 1]
 };
 
-template <typename T, int DP> struct Ra {
+// WK wavefronts share a block's 128 / WK rows, each with its 32 rows of every tile of the other side
+template <typename T, int DP, int WK> struct Ra {
     static constexpr int EPC = Mm<T>::EPC, CHUNKS = DP / EPC, KS = DP / (2 * EPC), ES = (int)sizeof(T);
-    static constexpr int BN = ES == 2 ? 64 : 32;              // rows of a staged tile
+    static constexpr int BM = 128 / WK;
+    static constexpr int BN = WK > 1 ? 32 * WK : ES == 2 ? 64 : 32;      // rows of a staged tile
+    static constexpr int SUB = BN / (32 * WK);                // 32-row pieces of it that a wavefront takes
     static constexpr int PITCH = DP * ES + 32;                // rows 8 dwords apart in the banks: row-wise and column-wise reads are free of conflicts
     static constexpr int TILE = BN * PITCH;
     static constexpr int PER = BN * CHUNKS / RA_THREADS;      // chunks of a tile a thread brings
     static constexpr int DT = DP / 32;                        // 32-channel pieces of a head
 };
 
-// A tile on its way from memory to LDS, in registers meanwhile; rows from `rows` on and channels from d on are zeros and not read
-template <typename T, int DP> struct RaTile {
-    typedef Ra<T, DP> R;
+// Sixteen bytes of a row of d channels from channel c on, through a buffer whose end is the last row's: rows beyond are zeros.  Where d is no whole
+// number of chunks the last one is taken from the row's end (ra_shift puts it in its place).
+template <typename T> __device__ __forceinline__ unsigned ra_offset(int64_t row, int64_t ld, int c, int d) {
+    constexpr int EPC = Mm<T>::EPC;
+    if (c >= d) return 0xffffffffu;
+    return (unsigned)((row * ld + (c + EPC > d ? (d > EPC ? d - EPC : 0) : c)) * (int64_t)sizeof(T));
+}
+template <typename T> __device__ __forceinline__ __amdgpu_buffer_rsrc_t ra_buffer(const T* base, int64_t ld, int rows, int d) {
+    const unsigned bytes = rows > 0 ? (unsigned)(((int64_t)(rows - 1) * ld + d) * (int64_t)sizeof(T)) : 0u;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, bytes, 0x00020000);
+}
+typedef unsigned int ra_u4 __attribute__((ext_vector_type(4)));
+template <typename T> __device__ __forceinline__ uint4 ra_load(__amdgpu_buffer_rsrc_t r, unsigned off, int d) {
+    constexpr int EPC = Mm<T>::EPC;
+    if (d >= EPC) {
+        const ra_u4 v = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
+        return make_uint4(v.x, v.y, v.z, v.w);
+    }
+    unsigned e[4] = {0, 0, 0, 0};          // heads narrower than a chunk, element by element
+#pragma unroll
+    for (int k = 0; k < EPC; ++k) {
+        if (k >= d) break;
+        const unsigned o = off == 0xffffffffu ? off : off + k * (unsigned)sizeof(T);
+        if (sizeof(T) == 2) e[k >> 1] |= (unsigned)(unsigned short)__builtin_amdgcn_raw_buffer_load_b16(r, o, 0, 0) << (16 * (k & 1));
+        else e[k] = __builtin_amdgcn_raw_buffer_load_b32(r, o, 0, 0);
+    }
+    return make_uint4(e[0], e[1], e[2], e[3]);
+}
+template <typename T> __device__ __forceinline__ uint4 ra_shift(uint4 v, int c, int d) {
+    constexpr int EPC = Mm<T>::EPC;
+    const int s = c + EPC > d && c < d && d > EPC ? (c + EPC - d) * 8 * (int)sizeof(T) : 0;
+    uint64_t lo = v.x | (uint64_t)v.y << 32, hi = v.z | (uint64_t)v.w << 32;
+    lo = s >= 64 ? hi >> (s & 63) : s ? lo >> s | hi << (64 - s) : lo;
+    hi = s >= 64 ? 0 : hi >> s;
+    return make_uint4((unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32));
+}
+
+// A tile on its way from memory to LDS, in registers meanwhile
+template <typename T, typename R> struct RaTile {
     uint4 v[R::PER];
-    __device__ __forceinline__ void load(const T* base, int64_t ld, int row0, int rows, int d) {
+    unsigned off[R::PER];
+    __device__ __forceinline__ void place(int64_t ld, int d) {
 #pragma unroll
         for (int i = 0; i < R::PER; ++i) {
-            const int at = i * RA_THREADS + (int)threadIdx.x, r = at / R::CHUNKS, c = (at - r * R::CHUNKS) * R::EPC;
-            const bool there = row0 + r < rows && c < d;
-            v[i] = ld16(there ? base + (int64_t)(row0 + r) * ld + c : base, there ? d - c : 0);
+            const int at = i * RA_THREADS + (int)threadIdx.x, r = at / R::CHUNKS;
+            off[i] = ra_offset<T>(r, ld, (at - r * R::CHUNKS) * R::EPC, d);
         }
     }
-    __device__ __forceinline__ void store(unsigned char* lds) const {
+    // rows row0 .. of `rows`
+    __device__ __forceinline__ void load(const T* base, int64_t ld, int row0, int rows, int d) {
+        const auto buf = ra_buffer(base + (int64_t)row0 * ld, ld, min(rows - row0, R::BN), d);
+#pragma unroll
+        for (int i = 0; i < R::PER; ++i) v[i] = ra_load<T>(buf, off[i], d);
+    }
+    __device__ __forceinline__ void store(unsigned char* lds, int d) {
+        if (d % R::EPC) {
+#pragma unroll
+            for (int i = 0; i < R::PER; ++i) v[i] = ra_shift<T>(v[i], (i * RA_THREADS + (int)threadIdx.x) % R::CHUNKS * R::EPC, d);
+        }
 #pragma unroll
         for (int i = 0; i < R::PER; ++i) {
             const int at = i * RA_THREADS + (int)threadIdx.x, r = at / R::CHUNKS, c = at - r * R::CHUNKS;
@@ -72,22 +122,25 @@ template <typename T, int DP> struct RaTile {
         }
     }
 };
-// a wavefront's 32 rows as an operand: the lane's row, its half of every 2 * EPC channels
-template <typename T, int DP> struct RaRows {
-    typedef Ra<T, DP> R;
+// a wavefront's 32 rows as an operand: the lane's row (below `rows`, or zeros), its half of every 2 * EPC channels
+template <typename T, typename R> struct RaRows {
     uint4 v[R::KS];
-    __device__ __forceinline__ void load(const T* row, bool there, int d, int g) {
+    __device__ __forceinline__ void load(const T* base, int64_t ld, int64_t row, bool there, int rows, int d, int g) {
+        const auto buf = ra_buffer(base, ld, rows, d);
 #pragma unroll
         for (int s = 0; s < R::KS; ++s) {
             const int c = (2 * s + g) * R::EPC;
-            v[s] = ld16(there && c < d ? row + c : row, there ? d - c : 0);
+            v[s] = ra_load<T>(buf, there ? ra_offset<T>(row, ld, c, d) : 0xffffffffu, d);
+        }
+        if (d % R::EPC) {
+#pragma unroll
+            for (int s = 0; s < R::KS; ++s) v[s] = ra_shift<T>(v[s], (2 * s + g) * R::EPC, d);
         }
     }
 };
 // rows row .. row + 31 of a tile times such rows: result[tile row][own row]
-template <typename T, int DP>
-__device__ __forceinline__ mm_f16 ra_products(const unsigned char* tile, int row, const RaRows<T, DP>& own, int lane) {
-    typedef Ra<T, DP> R;
+template <typename T, typename R>
+__device__ __forceinline__ mm_f16 ra_products(const unsigned char* tile, int row, const RaRows<T, R>& own, int lane) {
     mm_f16 acc = {};
     const unsigned char* p = tile + (row + (lane & 31)) * R::PITCH + (lane >> 5) * 16;
 #pragma unroll
@@ -95,9 +148,8 @@ __device__ __forceinline__ mm_f16 ra_products(const unsigned char* tile, int row
     return acc;
 }
 // out[t][channel 32 t + .][own row] += sum over the tile's rows row .. row + 31 of tile[row][channel] w[row][own row], w as a result lies
-template <typename T, int DP>
-__device__ __forceinline__ void ra_mix(const unsigned char* tile, int row, const float (&w)[16], mm_f16 (&out)[DP / 32], int lane) {
-    typedef Ra<T, DP> R;
+template <typename T, typename R>
+__device__ __forceinline__ void ra_mix(const unsigned char* tile, int row, const float (&w)[16], mm_f16 (&out)[R::DT], int lane) {
 #pragma unroll
     for (int u = 0; u < 16 / R::EPC; ++u) {
         const uint4 b = Mm<T>::pack(w + u * R::EPC);
@@ -115,39 +167,76 @@ __device__ __forceinline__ void ra_store4(T* p, int n, const float (&v)[4]) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) if (k < n) p[k] = e[k];
 }
+// channel of register r of piece t
+__device__ __forceinline__ int ra_channel(int t, int r, int g) { return 32 * t + 4 * g + 2 * r; }
+
+// Sums over the WK wavefronts that share rows, by pieces of 32 channels: afterwards wavefront wk holds the sums of the pieces t with t % WK == wk.  `area`
+// is no longer read by anybody; every wavefront calls.
+template <typename R, int WK>
+__device__ __forceinline__ void ra_gather(mm_f16 (&out)[R::DT], float* area, int wq, int wk, int lane) {
+    if (WK == 1) return;
+    float* mine = area + (int64_t)(wq * WK) * R::DT * 1024;
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < R::DT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            *reinterpret_cast<float4*>(mine + ((wk * R::DT + t) * 4 + r) * 256 + lane * 4) = make_float4(out[t][4 * r], out[t][4 * r + 1], out[t][4 * r + 2], out[t][4 * r + 3]);
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < R::DT; ++t) {
+        if (t % WK != wk) continue;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < WK; ++w) {
+                const float4 v = *reinterpret_cast<const float4*>(mine + ((w * R::DT + t) * 4 + r) * 256 + lane * 4);
+                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+            }
+            out[t][4 * r] = s.x; out[t][4 * r + 1] = s.y; out[t][4 * r + 2] = s.z; out[t][4 * r + 3] = s.w;
+        }
+    }
+}
 
 __device__ __forceinline__ int ra_clamp(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
 __device__ __forceinline__ int ra_keys(const AttnArgs& a, int n) { return a.len ? ra_clamp(a.len[n], 0, a.pk) : a.pk; }
 __device__ __forceinline__ int ra_start(const AttnArgs& a, int n) { return a.start ? ra_clamp(a.start[n], -(1 << 29), 1 << 29) : 0; }
+__device__ __forceinline__ bool ra_any(bool v) {
+#ifdef __HIP__
+    return __builtin_amdgcn_ballot_w64(v) != 0;
+#else
+    int s = v;
+    for (int o = 1; o < 64; o <<= 1) s |= __shfl_xor(s, o, 64);
+    return s != 0;
+#endif
+}
 
-// The bias of head h by distance, lut[rel + reach + RA_PAD], in units of log2.  Finite values stay finite (a mask of the type's lowest value
-// leaves a row of such values with equal probabilities, as the formula does).
-__device__ __forceinline__ void ra_bias(const AttnArgs& a, int h, float* lut) {
-    for (int t = threadIdx.x; t < 2 * a.reach + 1 + 2 * RA_PAD; t += RA_THREADS) {
-        float b = 0.f;
-        if (a.table) {
-            b = a.table[(int64_t)h * a.nb + ra_clamp(a.map[ra_clamp(t - RA_PAD, 0, 2 * a.reach)], 0, a.nb - 1)];
-            const float big = 3.402823466e38f;
-            b = fabsf(b) <= big ? fminf(fmaxf(b * RA_LOG2E, -big), big) : b;
+// The bias of `heads` heads from h on by distance, lut[head][rel + reach + RA_PAD], in units of log2.  Finite values stay finite (a mask of the type's
+// lowest value leaves a row of such values with equal probabilities, as the formula does).
+__host__ __device__ inline int ra_lut(int reach) { return 2 * reach + 1 + 2 * RA_PAD; }
+__device__ __forceinline__ void ra_bias(const AttnArgs& a, int h, int heads, float* lut) {
+    const int n = ra_lut(a.reach);
+    for (int t = threadIdx.x; t < n; t += RA_THREADS) {
+        const int id = a.table ? ra_clamp(a.map[ra_clamp(t - RA_PAD, 0, 2 * a.reach)], 0, a.nb - 1) : 0;
+        for (int k = 0; k < heads; ++k) {
+            float b = 0.f;
+            if (a.table) {
+                b = a.table[(int64_t)(h + k) * a.nb + id];
+                const float big = 3.402823466e38f;
+                b = fabsf(b) <= big ? fminf(fmaxf(b * RA_LOG2E, -big), big) : b;
+            }
+            lut[k * n + t] = b;
         }
-        lut[t] = b;
     }
 }
+// whether all distances relmin .. relmax have one bias
+__device__ __forceinline__ bool ra_far(int reach, int relmin, int relmax) { return relmax <= -reach || relmin >= reach; }
 
-// The bias of a 32-row tile (keys or queries row0 ..) for this lane: 16 values at compile-time distances from one place, or one value
-struct RaBias {
-    const float* at;      // NULL: `far` everywhere
-    float far;
-};
-// relmin, relmax: the least and largest distance of the wavefront's tile; rel: that of the lane's element 0
-__device__ __forceinline__ RaBias ra_tile_bias(const float* lut, int reach, int relmin, int relmax, int rel) {
-    if (relmax <= -reach) return {nullptr, lut[RA_PAD]};
-    if (relmin >= reach) return {nullptr, lut[RA_PAD + 2 * reach]};
-    return {lut + rel + reach + RA_PAD, 0.f};
-}
+__host__ __device__ inline int64_t ra_distances(int reach) { return 2 * (int64_t)reach + 1; }
 
 struct RaBlock { int n, h, tile, split; };
-__device__ __forceinline__ RaBlock ra_block(const AttnArgs& a, int heads, int tiles, int splits) {
+__device__ __forceinline__ RaBlock ra_block(int heads, int tiles, int splits) {
     const int b = xcd_remap((int)blockIdx.x, (int)gridDim.x);
     RaBlock r;
     r.split = b % splits;
@@ -158,147 +247,193 @@ __device__ __forceinline__ RaBlock ra_block(const AttnArgs& a, int heads, int ti
     return r;
 }
 
-// KEEP (a backward pass follows, bfloat16): p enters its product as two terms, and y is kept with what its rounding takes away.  In the gradient of
-// the table most of ds cancels, and delta's error does not: with p of 8 bits the sum of a bucket is off by 3e-4, with 16 by 1e-6.
-template <typename T, int DP, bool KEEP>
+template <typename T, int DP, int WK>
 __global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
-    typedef Ra<T, DP> R;
+    typedef Ra<T, DP, WK> R;
     extern __shared__ __attribute__((aligned(16))) unsigned char ra_lds[];
     unsigned char *kt = ra_lds, *vt = ra_lds + R::TILE;
     float* lut = reinterpret_cast<float*>(ra_lds + 2 * R::TILE);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 31, g = lane >> 5;
-    const int tiles = (a.pq + RA_BM - 1) / RA_BM;
-    RaBlock b = ra_block(a, a.H, tiles, a.splits);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 31, g = lane >> 5, wq = wave / WK, wk = wave % WK;
+    const int share = a.H / a.G, rows = a.fold ? share * a.pq : a.pq, tiles = (rows + R::BM - 1) / R::BM;
+    RaBlock b = ra_block(a.fold ? a.G : a.H, tiles, a.splits);
     if (a.causal) b.tile = tiles - 1 - b.tile;             // (the blocks with the most keys first)
-    const int n = b.n, h = b.h, hk = h / (a.H / a.G);
-    const int i0 = b.tile * RA_BM + wave * 32, i = min(i0 + l, a.pq - 1);
-    const bool work = i0 < a.pq;
-    const int start = ra_start(a, n), keys = ra_keys(a, n), qmin = i0 + start, qmax = min(i0 + 31, a.pq - 1) + start, qpos = i + start;
+    const int n = b.n, hk = a.fold ? b.h : b.h / share, h0 = a.fold ? hk * share : b.h;
+    const int r0 = b.tile * R::BM + wq * 32, r = min(r0 + l, rows - 1);
+    const int hh = a.fold ? r / a.pq : 0, i = r - hh * a.pq, h = h0 + hh;
+    const bool work = r0 < rows;
+    const int start = ra_start(a, n), keys = ra_keys(a, n), qpos = i + start;
+    const int qmin = (a.fold ? 0 : r0) + start, qmax = (a.fold ? a.pq - 1 : min(r0 + 31, a.pq - 1)) + start;
     const T* kb = (const T*)a.k + (int64_t)n * a.pk * a.ldk + (int64_t)hk * a.d;
     const T* vb = (const T*)a.v + (int64_t)n * a.pk * a.ldv + (int64_t)hk * a.d;
     int end = keys;
-    if (a.causal) end = ra_clamp(min(b.tile * RA_BM + RA_BM, a.pq) + start, 0, keys);
+    if (a.causal) end = ra_clamp((a.fold ? a.pq : min(b.tile * R::BM + R::BM, a.pq)) + start, 0, keys);
     const int all = (end + R::BN - 1) / R::BN, per = (all + a.splits - 1) / a.splits, t0 = b.split * per, t1 = min(all, t0 + per);
-    RaTile<T, DP> kr, vr;
+    RaTile<T, R> kr, vr;
+    kr.place(a.ldk, a.d);
+    vr.place(a.ldv, a.d);
     if (t0 < t1) { kr.load(kb, a.ldk, t0 * R::BN, end, a.d); vr.load(vb, a.ldv, t0 * R::BN, end, a.d); }
-    RaRows<T, DP> qr;
-    qr.load((const T*)a.q + ((int64_t)n * a.pq + i) * a.ldq + (int64_t)h * a.d, work, a.d, g);
-    ra_bias(a, h, lut);
+    RaRows<T, R> qr;
+    if (a.fold)                             // (rows of other heads lie d elements apart: from the sample's first query on)
+        qr.load((const T*)a.q + ((int64_t)n * a.pq + i) * a.ldq + (int64_t)h * a.d, 0, 0, work, 1, a.d, g);
+    else
+        qr.load((const T*)a.q + ((int64_t)n * a.pq + r0) * a.ldq + (int64_t)h * a.d, a.ldq, i - r0, work, min(32, a.pq - r0), a.d, g);
+    ra_bias(a, h0, a.fold ? share : 1, lut);
+    lut += hh * ra_lut(a.reach);
     mm_f16 o[R::DT] = {};
     float top = -INFINITY, sum = 0.f;
     for (int t = t0; t < t1; ++t) {
         __syncthreads();
-        kr.store(kt);
-        vr.store(vt);
+        kr.store(kt, a.d);
+        vr.store(vt, a.d);
         __syncthreads();
         if (t + 1 < t1) { kr.load(kb, a.ldk, (t + 1) * R::BN, end, a.d); vr.load(vb, a.ldv, (t + 1) * R::BN, end, a.d); }
-        const int j0 = t * R::BN;
-        if (!work || (a.causal && j0 > qmax)) continue;
-        const bool edge = j0 + R::BN > keys || (a.causal && j0 + R::BN - 1 > qmin);
-        float s[R::BN / 32][16];
-        const RaBias bias = ra_tile_bias(lut, a.reach, j0 - qmax, j0 + R::BN - 1 - qmin, j0 + 4 * g - qpos);
+        const int j0 = t * R::BN + wk * 32 * R::SUB;       // the wavefront's keys of the tile
+        if (!work || j0 >= end || (a.causal && j0 > qmax)) continue;
+        const int last = j0 + 32 * R::SUB - 1;
+        const bool edge = last >= keys || (a.causal && last > qmin);
+        float s[R::SUB][16];
         float mx = -INFINITY;
+        const bool far = ra_far(a.reach, j0 - qmax, last - qmin);
+        const float one = lut[RA_PAD + (j0 - qmax >= a.reach ? 2 * a.reach : 0)];
+        const float* near = lut + (far ? 0 : j0 + 4 * g - qpos + a.reach + RA_PAD);
 #pragma unroll
-        for (int u = 0; u < R::BN / 32; ++u) {
-            const mm_f16 acc = ra_products<T, DP>(kt, 32 * u, qr, lane);
+        for (int u = 0; u < R::SUB; ++u) {
+            const mm_f16 acc = ra_products<T, R>(kt, wk * 32 * R::SUB + 32 * u, qr, lane);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                float v = fmaf(acc[r], a.scale2, bias.at ? bias.at[32 * u + (r & 3) + 8 * (r >> 2)] : bias.far);
-                if (edge) {
-                    const int j = j0 + 32 * u + 4 * g + (r & 3) + 8 * (r >> 2);
-                    if (j >= keys || (a.causal && j > qpos)) v = -INFINITY;
-                }
-                s[u][r] = v;
-                mx = fmaxf(mx, v);
-            }
+            for (int e = 0; e < 16; ++e) s[u][e] = acc[e];
         }
+        if (far) {
+#pragma unroll
+            for (int u = 0; u < R::SUB; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[u][e] = fmaf(s[u][e], a.scale2, one);
+        } else {
+#pragma unroll
+            for (int u = 0; u < R::SUB; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[u][e] = fmaf(s[u][e], a.scale2, near[32 * u + (e & 3) + 8 * (e >> 2)]);
+        }
+        if (edge) {
+            const int least = a.causal ? min(keys - 1, qpos) : keys - 1;      // the last key that this query sees
+#pragma unroll
+            for (int u = 0; u < R::SUB; ++u)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) if (j0 + 32 * u + 4 * g + (e & 3) + 8 * (e >> 2) > least) s[u][e] = -INFINITY;
+        }
+#pragma unroll
+        for (int u = 0; u < R::SUB; ++u)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[u][e]);
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        mx = fmaxf(mx, top);
-        const float base = mx == -INFINITY ? 0.f : mx, shrink = exp2_fast(top - base);
-        top = mx;
+        // the reference moves only where a row's maximum has passed it by 2^8 (or it had none): until then p is up to 2^8, which float and
+        // bfloat16 hold as exactly as 1
+        if (ra_any(mx > top + 8.f || (top == -INFINITY && mx > top))) {
+            const float to = fmaxf(mx, top), base = to == -INFINITY ? 0.f : to, shrink = exp2_fast(top - base);
+            top = to;
+            sum *= shrink;
+#pragma unroll
+            for (int c = 0; c < R::DT; ++c)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[c][e] *= shrink;
+        }
+        const float base = top == -INFINITY ? 0.f : top;
         float part = 0.f;
 #pragma unroll
-        for (int u = 0; u < R::BN / 32; ++u)
+        for (int u = 0; u < R::SUB; ++u)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) { s[u][r] = exp2_fast(s[u][r] - base); part += s[u][r]; }
-        sum = fmaf(sum, shrink, part);
-#pragma unroll
-        for (int c = 0; c < R::DT; ++c)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[c][r] *= shrink;
+            for (int e = 0; e < 16; ++e) { s[u][e] = exp2_fast(s[u][e] - base); part += s[u][e]; }
+        sum += part;
         // (p enters the product in the element type: for bfloat16 an error of 2^-9 of each term, below the rounding of y)
 #pragma unroll
-        for (int u = 0; u < R::BN / 32; ++u) {
-            ra_mix<T, DP>(vt, 32 * u, s[u], o, lane);
-            if constexpr (KEEP && R::ES == 2) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[u][r] -= bf2f(f2bf(s[u][r]));
-                ra_mix<T, DP>(vt, 32 * u, s[u], o, lane);
-            }
-        }
+        for (int u = 0; u < R::SUB; ++u) ra_mix<T, R>(vt, wk * 32 * R::SUB + 32 * u, s[u], o, lane);
     }
     sum += __shfl_xor(sum, 32, 64);
-    if (i0 + l >= a.pq) return;
-    const int64_t row = ((int64_t)n * a.H + h) * a.pq + i;
-    if (a.splits > 1) {
-        const int64_t rows = (int64_t)a.m * a.H * a.pq, at = b.split * rows + row;
-        if (g == 0) { a.part_ml[2 * at] = top; a.part_ml[2 * at + 1] = sum; }
+    if (WK > 1) {                           // one reference for the wavefronts that share the rows
+        float* red = reinterpret_cast<float*>(ra_lds);
+        __syncthreads();
+        if (g == 0) { red[(wave * 32 + l) * 2] = top; red[(wave * 32 + l) * 2 + 1] = sum; }
+        __syncthreads();
+        float to = -INFINITY, all_sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < WK; ++w) to = fmaxf(to, red[((wq * WK + w) * 32 + l) * 2]);
+        const float base = to == -INFINITY ? 0.f : to;
+#pragma unroll
+        for (int w = 0; w < WK; ++w) all_sum = fmaf(red[((wq * WK + w) * 32 + l) * 2 + 1], exp2_fast(red[((wq * WK + w) * 32 + l) * 2] - base), all_sum);
+        const float shrink = exp2_fast(top - base);
 #pragma unroll
         for (int c = 0; c < R::DT; ++c)
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int ch = 32 * c + 4 * g + 2 * r;
-                const float v[4] = {o[c][r], o[c][r + 1], o[c][r + 2], o[c][r + 3]};
+            for (int e = 0; e < 16; ++e) o[c][e] *= shrink;
+        top = to;
+        sum = all_sum;
+        ra_gather<R, WK>(o, reinterpret_cast<float*>(ra_lds), wq, wk, lane);
+    }
+    if (r0 + l >= rows) return;
+    const int64_t row = ((int64_t)n * a.H + h) * a.pq + i;
+    if (a.splits > 1) {
+        const int64_t at = b.split * ((int64_t)a.m * a.H * a.pq) + row;
+        if (g == 0 && wk == 0) { a.part_ml[2 * at] = top; a.part_ml[2 * at + 1] = sum; }
+#pragma unroll
+        for (int c = 0; c < R::DT; ++c) {
+            if (c % WK != wk) continue;
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const int ch = ra_channel(c, e, g);
+                const float v[4] = {o[c][e], o[c][e + 1], o[c][e + 2], o[c][e + 3]};
                 if (ch < a.d) ra_store4(a.part + at * a.d + ch, a.d - ch, v);
             }
+        }
         return;
     }
     const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
-    if (KEEP && g == 0) a.stats[row] = {top, sum == 0.f ? -INFINITY : -log2f(sum)};
+    if (a.stats && g == 0 && wk == 0) a.stats[row] = {top, sum == 0.f ? -INFINITY : -log2f(sum)};
     T* yr = (T*)a.y + ((int64_t)n * a.pq + i) * a.ldy + (int64_t)h * a.d;
-    bf16_t* low = a.low ? a.low + ((int64_t)n * a.pq + i) * a.H * a.d + (int64_t)h * a.d : nullptr;
 #pragma unroll
-    for (int c = 0; c < R::DT; ++c)
+    for (int c = 0; c < R::DT; ++c) {
+        if (c % WK != wk) continue;
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const int ch = 32 * c + 4 * g + 2 * r;
-            if (ch >= a.d) continue;
-            float v[4] = {o[c][r] * inv, o[c][r + 1] * inv, o[c][r + 2] * inv, o[c][r + 3] * inv};
-            ra_store4(yr + ch, a.d - ch, v);
-            if (KEEP && R::ES == 2) {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] -= bf2f(f2bf(v[k]));
-                ra_store4(low + ch, a.d - ch, v);
-            }
+        for (int e = 0; e < 16; e += 4) {
+            const int ch = ra_channel(c, e, g);
+            const float v[4] = {o[c][e] * inv, o[c][e + 1] * inv, o[c][e + 2] * inv, o[c][e + 3] * inv};
+            if (ch < a.d) ra_store4(yr + ch, a.d - ch, v);
         }
+    }
 }
 
-// Joins the parts of a row: a wavefront per row, a lane per channel
+// Joins the parts of a row: a wavefront per row; lane s knows part s's weight, then a lane has a channel
+constexpr int RA_MAX_SPLITS = 32;
 template <typename T>
 __global__ void __launch_bounds__(RA_THREADS) relattn_join(AttnArgs a) {
     const int lane = threadIdx.x & 63;
     const int64_t rows = (int64_t)a.m * a.H * a.pq, row = (int64_t)blockIdx.x * RA_WAVES + (threadIdx.x >> 6);
     if (row >= rows) return;
-    float top = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_ml[2 * (s * rows + row)]);
-    const float base = top == -INFINITY ? 0.f : top;
-    float sum = 0.f;
-    for (int s = 0; s < a.splits; ++s) sum = fmaf(a.part_ml[2 * (s * rows + row) + 1], exp2_fast(a.part_ml[2 * (s * rows + row)] - base), sum);
+    float top = -INFINITY, sum = 0.f;
+    if (lane < a.splits) { top = a.part_ml[2 * (lane * rows + row)]; sum = a.part_ml[2 * (lane * rows + row) + 1]; }
+    float to = top;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) to = fmaxf(to, __shfl_xor(to, o, 64));
+    const float weight = exp2_fast(top - (to == -INFINITY ? 0.f : to));
+    sum *= weight;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
     const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
-    if (a.stats && lane == 0) a.stats[row] = {top, sum == 0.f ? -INFINITY : -log2f(sum)};
+    if (a.stats && lane == 0) a.stats[row] = {to, sum == 0.f ? -INFINITY : -log2f(sum)};
     const int64_t nh = row / a.pq;
     const int i = (int)(row - nh * a.pq), h = (int)(nh % a.H), n = (int)(nh / a.H);
     T* yr = (T*)a.y + ((int64_t)n * a.pq + i) * a.ldy + (int64_t)h * a.d;
-    for (int c = lane; c < a.d; c += 64) {
-        float v = 0.f;
-        for (int s = 0; s < a.splits; ++s) v = fmaf(a.part[(s * rows + row) * a.d + c], exp2_fast(a.part_ml[2 * (s * rows + row)] - base), v);
-        v *= inv;
-        st(yr, c, v);
-        if (sizeof(T) == 2 && a.low) st(a.low, ((int64_t)n * a.pq + i) * a.H * a.d + (int64_t)h * a.d + c, v - bf2f(f2bf(v)));
+    float v[2] = {0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s) {
+        const float w = __shfl(weight, s, 64);
+        const float* p = a.part + (s * rows + row) * a.d;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) if (lane + 64 * k < a.d) v[k] = fmaf(p[lane + 64 * k], w, v[k]);
     }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) if (lane + 64 * k < a.d) st(yr, lane + 64 * k, v[k] * inv);
 }
 
-// Sums of ds along the diagonals, carried over a wavefront's tiles of 32 keys (its 32 queries stay): `held` is this lane's sum for distance rel0 + lane
+// Sums of ds along the diagonals of a wavefront's 32 x 32 tiles (its queries stay, its keys ascend): `held` is this lane's sum for distance rel0 + lane.
+// What tiles that follow each other share is carried; every distance is stored once.
 struct RaDiagonals {
     float lo = 0.f, hi = 0.f, held = 0.f;      // distances of -reach and below, reach and above; the carried one
     int rel0 = 0, from = 0, to = 0;            // distances from .. to - 1 are stored
@@ -322,18 +457,18 @@ struct RaDiagonals {
         held = 0.f;
         carrying = false;
     }
-    // ds of keys j0 .. j0 + 31 (positions) by queries q0 .. q0 + 31: relmin = j0 - q0 - 31
+    // a tile whose key 0 is relmin + 31 positions behind its query 0, not wholly beyond the reach
     __device__ __forceinline__ void add(const float (&ds)[16], int relmin, float* area, int lane) {
-        if (relmin + 62 <= -reach || relmin >= reach) {
-            flush(lane);
-            float s = 0.f;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s += ds[r];
-            if (relmin >= reach) hi += s; else lo += s;
-            return;
-        }
         const int l = lane & 31, g = lane >> 5;
-        if (!carrying) rel0 = relmin, carrying = true;
+        if (!carrying || rel0 != relmin) {
+            flush(lane);
+            if (stored) {                      // (distances that no tile of this wavefront meets)
+                for (int rel = to + lane; rel < min(relmin, reach); rel += 64) line[rel + reach] = 0.f;
+                to = max(to, min(relmin, reach));
+            }
+            rel0 = relmin;
+            carrying = true;
+        }
         // line D of the area: the pairs of distance relmin + D, by query; lines hold zeros where there is no such pair
 #pragma unroll
         for (int r = 0; r < 16; ++r) area[((r & 3) + 8 * (r >> 2) + 4 * g + 31 - l) * RA_DIAG_PITCH + l] = ds[r];
@@ -368,147 +503,218 @@ struct RaDiagonals {
     }
 };
 
-// dq of 128 queries, their delta, and the wavefronts' sums of ds by distance
-template <typename T, int DP>
+// dq of a block's queries, their delta, and the wavefronts' sums of ds by distance.
+// delta: dy . y has the rounding of a bfloat16 y in it.  dq and dk do not mind, but in the sums over buckets most of ds cancels, and that error does not.  So
+// the sum of a row's ds, which is 0 but for delta's error, corrects it: the sums of tiles beyond the reach afterwards, with those of p beside them,
+// while the tiles within the reach are gone through once more.  (Float: y is as exact as the rest, one walk does it all.)
+template <typename T, int DP, int WK>
 __global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_q(AttnArgs a) {
-    typedef Ra<T, DP> R;
+    typedef Ra<T, DP, WK> R;
     extern __shared__ __attribute__((aligned(16))) unsigned char ra_lds[];
     unsigned char *kt = ra_lds, *vt = ra_lds + R::TILE;
-    float* area = reinterpret_cast<float*>(ra_lds + 2 * R::TILE) + (threadIdx.x >> 6) * 63 * RA_DIAG_PITCH;
-    float* lut = reinterpret_cast<float*>(ra_lds + 2 * R::TILE) + RA_WAVES * 63 * RA_DIAG_PITCH;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 31, g = lane >> 5;
-    const int tiles = (a.pq + RA_BM - 1) / RA_BM;
-    RaBlock b = ra_block(a, a.H, tiles, 1);
+    float* areas = reinterpret_cast<float*>(ra_lds + 2 * R::TILE);
+    float* lut = areas + RA_WAVES * 63 * RA_DIAG_PITCH;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 31, g = lane >> 5, wq = wave / WK, wk = wave % WK;
+    float* area = areas + wave * 63 * RA_DIAG_PITCH;
+    const int tiles = (a.pq + R::BM - 1) / R::BM;
+    RaBlock b = ra_block(a.H, tiles, 1);
     if (a.causal) b.tile = tiles - 1 - b.tile;
     const int n = b.n, h = b.h, hk = h / (a.H / a.G);
-    const int i0 = b.tile * RA_BM + wave * 32, i = min(i0 + l, a.pq - 1);
+    const int i0 = b.tile * R::BM + wq * 32, i = min(i0 + l, a.pq - 1);
     const bool work = i0 < a.pq, mine = i0 + l < a.pq;
     const int start = ra_start(a, n), keys = ra_keys(a, n), qmin = i0 + start, qmax = min(i0 + 31, a.pq - 1) + start, qpos = i + start;
     const T* kb = (const T*)a.k + (int64_t)n * a.pk * a.ldk + (int64_t)hk * a.d;
     const T* vb = (const T*)a.v + (int64_t)n * a.pk * a.ldv + (int64_t)hk * a.d;
+    const int block_qmin = b.tile * R::BM + start, block_qmax = min(b.tile * R::BM + R::BM, a.pq) - 1 + start;
     int end = keys;
-    if (a.causal) end = ra_clamp(min(b.tile * RA_BM + RA_BM, a.pq) + start, 0, keys);
+    if (a.causal) end = ra_clamp(block_qmax + 1, 0, keys);
     const int all = (end + R::BN - 1) / R::BN;
-    RaTile<T, DP> kr, vr;
+    RaTile<T, R> kr, vr;
+    kr.place(a.ldk, a.d);
+    vr.place(a.ldv, a.d);
     if (all > 0) { kr.load(kb, a.ldk, 0, end, a.d); vr.load(vb, a.ldv, 0, end, a.d); }
-    const int64_t row = ((int64_t)n * a.H + h) * a.pq + i, place = ((int64_t)n * a.pq + i) * a.ldy + (int64_t)h * a.d;
-    RaRows<T, DP> qr, gr;
-    qr.load((const T*)a.q + ((int64_t)n * a.pq + i) * a.ldq + (int64_t)h * a.d, mine, a.d, g);
-    gr.load((const T*)a.dy + place, mine, a.d, g);
-    // delta: y with what its rounding took away, or the sum over a bucket, in which most of ds cancels, would lose half of its digits
+    const int64_t row = ((int64_t)n * a.H + h) * a.pq + i, first = ((int64_t)n * a.pq + i0) * a.ldy + (int64_t)h * a.d;
+    RaRows<T, R> qr, gr;
+    qr.load((const T*)a.q + ((int64_t)n * a.pq + i0) * a.ldq + (int64_t)h * a.d, a.ldq, l, mine, min(32, a.pq - i0), a.d, g);
+    gr.load((const T*)a.dy + first, a.ldy, l, mine, min(32, a.pq - i0), a.d, g);
     float delta = 0.f;
-    if (work) {
-        const T* yr = (const T*)a.y + place;
-        const bf16_t* low = a.low ? a.low + (((int64_t)n * a.pq + i) * a.H + h) * a.d : nullptr;
+    {
+        RaRows<T, R> yr;
+        yr.load((const T*)a.y + first, a.ldy, l, mine, min(32, a.pq - i0), a.d, g);
 #pragma unroll
         for (int s = 0; s < R::KS; ++s) {
-            const int c = (2 * s + g) * R::EPC;
-            T e[R::EPC];
+            T e[R::EPC], f[R::EPC];
             __builtin_memcpy(e, &gr.v[s], 16);
+            __builtin_memcpy(f, &yr.v[s], 16);
 #pragma unroll
-            for (int k = 0; k < R::EPC; ++k)
-                if (c + k < a.d) delta = fmaf(ld(e, k), ld(yr, c + k) + (low ? ld(low, c + k) : 0.f), delta);
+            for (int k = 0; k < R::EPC; ++k) delta = fmaf(ld(e, k), ld(f, k), delta);
         }
     }
     delta += __shfl_xor(delta, 32, 64);
-    if (mine && g == 0) a.delta[row] = delta;
     const float2_ stat = mine ? a.stats[row] : float2_{0.f, -INFINITY};
-    const float top = stat.y == -INFINITY ? 0.f : stat.x;
-    ra_bias(a, h, lut);
+    const bool some = stat.y != -INFINITY;                 // the query sees a key
+    const float top = some ? stat.x : 0.f;
+    const int least = !some ? -1 : a.causal ? min(keys - 1, qpos) : keys - 1;
+    ra_bias(a, h, 1, lut);
     for (int t = lane; t < 63 * RA_DIAG_PITCH; t += 64) area[t] = 0.f;
     RaDiagonals dg;
     dg.reach = a.reach;
-    dg.line = a.diag ? a.diag + (((int64_t)n * a.H + h) * ((a.pq + 31) / 32) + i0 / 32) * (2 * a.reach + 1) : nullptr;
+    dg.line = a.diag ? a.diag + (((int64_t)n * a.H + h) * tiles * RA_WAVES + b.tile * RA_WAVES + wave) * ra_distances(a.reach) : nullptr;
     mm_f16 dq[R::DT] = {};
+    float rowsum = 0.f, far_lo = 0.f, far_hi = 0.f;        // sums of ds over the row, of p beyond the reach on either side
+    // p (dp - delta) of one 32 x 32 tile, and p's sum
+    auto scores = [&](int at, int j0, float (&ds)[16], float& psum) __attribute__((always_inline)) {
+        const mm_f16 s = ra_products<T, R>(kt, at, qr, lane), dp = ra_products<T, R>(vt, at, gr, lane);
+        const bool far = ra_far(a.reach, j0 - qmax, j0 + 31 - qmin);
+        const float one = lut[RA_PAD + (j0 - qmax >= a.reach ? 2 * a.reach : 0)];
+        const float* near = lut + (far ? 0 : j0 + 4 * g - qpos + a.reach + RA_PAD);
+        float p[16];
+        if (far) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) p[e] = fmaf(s[e], a.scale2, one);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) p[e] = fmaf(s[e], a.scale2, near[(e & 3) + 8 * (e >> 2)]);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) p[e] = exp2_fast((p[e] - top) + stat.y);
+        if (j0 + 31 >= keys || i0 + 32 > a.pq || (a.causal && j0 + 31 > qmin) || ra_any(!some)) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const bool seen = j0 + 4 * g + (e & 3) + 8 * (e >> 2) <= least;
+                p[e] = seen ? p[e] : 0.f;
+                ds[e] = seen ? p[e] * (dp[e] - delta) : 0.f;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) ds[e] = p[e] * (dp[e] - delta);
+        }
+        psum = 0.f;
+        if (far) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) psum += p[e];
+        }
+        return far;
+    };
     for (int t = 0; t < all; ++t) {
         __syncthreads();
-        kr.store(kt);
-        vr.store(vt);
+        kr.store(kt, a.d);
+        vr.store(vt, a.d);
         __syncthreads();
         if (t + 1 < all) { kr.load(kb, a.ldk, (t + 1) * R::BN, end, a.d); vr.load(vb, a.ldv, (t + 1) * R::BN, end, a.d); }
 #pragma unroll 1
-        for (int u = 0; u < R::BN / 32; ++u) {
-            const int j0 = t * R::BN + 32 * u;
+        for (int u = 0; u < R::SUB; ++u) {
+            const int at = (wk * R::SUB + u) * 32, j0 = t * R::BN + at;
             if (!work || j0 >= end || (a.causal && j0 > qmax)) continue;
-            const bool edge = j0 + 32 > keys || i0 + 32 > a.pq || (a.causal && j0 + 31 > qmin);
-            const RaBias bias = ra_tile_bias(lut, a.reach, j0 - qmax, j0 + 31 - qmin, j0 + 4 * g - qpos);
-            const mm_f16 s = ra_products<T, DP>(kt, 32 * u, qr, lane), dp = ra_products<T, DP>(vt, 32 * u, gr, lane);
-            float ds[16];
+            float ds[16], psum;
+            const bool far = scores(at, j0, ds, psum);
+            if (dg.line) {
+                float s = 0.f;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float v = fmaf(s[r], a.scale2, bias.at ? bias.at[(r & 3) + 8 * (r >> 2)] : bias.far);
-                ds[r] = exp2_fast((v - top) + stat.y) * (dp[r] - delta);
-                if (edge) {
-                    const int j = j0 + 4 * g + (r & 3) + 8 * (r >> 2);
-                    if (!mine || j >= keys || (a.causal && j > qpos)) ds[r] = 0.f;
-                }
+                for (int e = 0; e < 16; ++e) s += ds[e];
+                rowsum += s;
+                if (far && j0 - qmax >= a.reach) { dg.hi += s; far_hi += psum; }
+                else if (far) { dg.lo += s; far_lo += psum; }
+                else if (R::ES == 4) dg.add(ds, j0 - qmin - 31, area, lane);
             }
-            if (stat.y == -INFINITY) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) ds[r] = 0.f;
-            }
-            if (dg.line) dg.add(ds, j0 - i0 - start - 31, area, lane);
-            ra_mix<T, DP>(kt, 32 * u, ds, dq, lane);
+            ra_mix<T, R>(kt, at, ds, dq, lane);
         }
     }
-    if (!work) return;
+    if (R::ES == 2 && dg.line) {
+        rowsum += __shfl_xor(rowsum, 32, 64);
+        if (WK > 1) {                       // ... over the wavefronts that share the row
+            __syncthreads();
+            float* red = reinterpret_cast<float*>(ra_lds);
+            if (g == 0) red[wave * 32 + l] = rowsum;
+            __syncthreads();
+            rowsum = 0.f;
+#pragma unroll
+            for (int w = 0; w < WK; ++w) rowsum += red[(wq * WK + w) * 32 + l];
+        }
+        delta += some ? rowsum : 0.f;
+        dg.lo = fmaf(-rowsum, far_lo, dg.lo);
+        dg.hi = fmaf(-rowsum, far_hi, dg.hi);
+        // the tiles with distances within the reach of some query of the block
+        const int t0 = ra_clamp(block_qmin - a.reach, 0, end) / R::BN, t1 = min(all, ra_clamp(block_qmax + a.reach, 0, end) / R::BN + 1);
+        if (t0 < t1) { kr.load(kb, a.ldk, t0 * R::BN, end, a.d); vr.load(vb, a.ldv, t0 * R::BN, end, a.d); }
+        for (int t = t0; t < t1; ++t) {
+            __syncthreads();
+            kr.store(kt, a.d);
+            vr.store(vt, a.d);
+            __syncthreads();
+            if (t + 1 < t1) { kr.load(kb, a.ldk, (t + 1) * R::BN, end, a.d); vr.load(vb, a.ldv, (t + 1) * R::BN, end, a.d); }
+#pragma unroll 1
+            for (int u = 0; u < R::SUB; ++u) {
+                const int at = (wk * R::SUB + u) * 32, j0 = t * R::BN + at;
+                if (!work || j0 >= end || (a.causal && j0 > qmax) || ra_far(a.reach, j0 - qmax, j0 + 31 - qmin)) continue;
+                float ds[16], psum;
+                scores(at, j0, ds, psum);
+                dg.add(ds, j0 - qmin - 31, area, lane);
+            }
+        }
+    }
+    if (mine && g == 0 && wk == 0) a.delta[row] = delta;
     if (dg.line) dg.finish(lane);
+    ra_gather<R, WK>(dq, reinterpret_cast<float*>(ra_lds), wq, wk, lane);
     if (!mine) return;
     T* out = (T*)a.dq + ((int64_t)n * a.pq + i) * a.ldq + (int64_t)h * a.d;
 #pragma unroll
-    for (int c = 0; c < R::DT; ++c)
+    for (int c = 0; c < R::DT; ++c) {
+        if (c % WK != wk) continue;
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const int ch = 32 * c + 4 * g + 2 * r;
-            const float v[4] = {dq[c][r] * a.scale, dq[c][r + 1] * a.scale, dq[c][r + 2] * a.scale, dq[c][r + 3] * a.scale};
+        for (int e = 0; e < 16; e += 4) {
+            const int ch = ra_channel(c, e, g);
+            const float v[4] = {dq[c][e] * a.scale, dq[c][e + 1] * a.scale, dq[c][e + 2] * a.scale, dq[c][e + 3] * a.scale};
             if (ch < a.d) ra_store4(out + ch, a.d - ch, v);
         }
+    }
 }
 
-// dk and dv of 128 keys: the queries of every head that shares them, one head after the other
-template <typename T, int DP>
+// dk and dv of a block's keys: the queries of every head that shares them, one head after the other
+template <typename T, int DP, int WK>
 __global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_kv(AttnArgs a) {
-    typedef Ra<T, DP> R;
+    typedef Ra<T, DP, WK> R;
     extern __shared__ __attribute__((aligned(16))) unsigned char ra_lds[];
     unsigned char *qt = ra_lds, *gt = ra_lds + R::TILE;
     float* rowv = reinterpret_cast<float*>(ra_lds + 2 * R::TILE);          // [3][BN]: top, -log2 sum, delta
     float* lut = rowv + 3 * R::BN;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 31, g = lane >> 5;
-    const int tiles = (a.pk + RA_BM - 1) / RA_BM;
-    const RaBlock b = ra_block(a, a.G, tiles, 1);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 31, g = lane >> 5, wq = wave / WK, wk = wave % WK;
+    const int tiles = (a.pk + R::BM - 1) / R::BM;
+    const RaBlock b = ra_block(a.G, tiles, 1);
     const int n = b.n, hk = b.h, share = a.H / a.G;
-    const int j0 = b.tile * RA_BM + wave * 32, j = min(j0 + l, a.pk - 1);
+    const int j0 = b.tile * R::BM + wq * 32, j = min(j0 + l, a.pk - 1);
     const int start = ra_start(a, n), keys = ra_keys(a, n);
     const bool work = j0 < keys, mine = j0 + l < keys;
-    RaRows<T, DP> kr, vr;
-    kr.load((const T*)a.k + ((int64_t)n * a.pk + j) * a.ldk + (int64_t)hk * a.d, mine, a.d, g);
-    vr.load((const T*)a.v + ((int64_t)n * a.pk + j) * a.ldv + (int64_t)hk * a.d, mine, a.d, g);
+    RaRows<T, R> kr, vr;
+    kr.load((const T*)a.k + ((int64_t)n * a.pk + j0) * a.ldk + (int64_t)hk * a.d, a.ldk, l, mine, min(32, keys - j0), a.d, g);
+    vr.load((const T*)a.v + ((int64_t)n * a.pk + j0) * a.ldv + (int64_t)hk * a.d, a.ldv, l, mine, min(32, keys - j0), a.d, g);
     mm_f16 dk[R::DT] = {}, dv[R::DT] = {};
-    const int first = a.causal ? ra_clamp(b.tile * RA_BM - start, 0, a.pq) : 0;       // no query before it sees one of the block's keys
-    const int t0 = first / R::BN, t1 = b.tile * RA_BM < keys ? (a.pq + R::BN - 1) / R::BN : 0;
+    const int first = a.causal ? ra_clamp(b.tile * R::BM - start, 0, a.pq) : 0;       // no query before it sees one of the block's keys
+    const int t0 = first / R::BN, t1 = b.tile * R::BM < keys ? (a.pq + R::BN - 1) / R::BN : 0;
+    RaTile<T, R> qs, gs;
+    qs.place(a.ldq, a.d);
+    gs.place(a.ldy, a.d);
     for (int hh = 0; hh < share; ++hh) {
         const int h = hk * share + hh;
         const T* qb = (const T*)a.q + (int64_t)n * a.pq * a.ldq + (int64_t)h * a.d;
         const T* gb = (const T*)a.dy + (int64_t)n * a.pq * a.ldy + (int64_t)h * a.d;
         const int64_t row0 = ((int64_t)n * a.H + h) * a.pq;
-        RaTile<T, DP> qs, gs;
         float2_ st = {0.f, -INFINITY};
         float dl = 0.f;
         auto load = [&](int t) __attribute__((always_inline)) {
             qs.load(qb, a.ldq, t * R::BN, a.pq, a.d);
             gs.load(gb, a.ldy, t * R::BN, a.pq, a.d);
-            st = {0.f, -INFINITY};
-            dl = 0.f;
-            const int i = t * R::BN + (int)threadIdx.x;
-            if ((int)threadIdx.x < R::BN && i < a.pq) { st = a.stats[row0 + i]; dl = a.delta[row0 + i]; }
+            const int i = min(t * R::BN + min((int)threadIdx.x, R::BN - 1), a.pq - 1);      // (rows beyond the last are masked)
+            st = a.stats[row0 + i];
+            dl = a.delta[row0 + i];
         };
         if (t0 < t1) load(t0);
         __syncthreads();                                   // (the bias of the head before has been read)
-        ra_bias(a, h, lut);
+        ra_bias(a, h, 1, lut);
         for (int t = t0; t < t1; ++t) {
             __syncthreads();
-            qs.store(qt);
-            gs.store(gt);
+            qs.store(qt, a.d);
+            gs.store(gt, a.d);
             if ((int)threadIdx.x < R::BN) {
                 rowv[threadIdx.x] = st.y == -INFINITY ? 0.f : st.x;
                 rowv[R::BN + threadIdx.x] = st.y;
@@ -517,47 +723,65 @@ __global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_kv(AttnArgs a) {
             __syncthreads();
             if (t + 1 < t1) load(t + 1);
 #pragma unroll 1
-            for (int u = 0; u < R::BN / 32; ++u) {
-                const int i0 = t * R::BN + 32 * u, qmin = i0 + start, qmax = min(i0 + 31, a.pq - 1) + start;
+            for (int u = 0; u < R::SUB; ++u) {
+                const int at = (wk * R::SUB + u) * 32, i0 = t * R::BN + at, qmin = i0 + start, qmax = min(i0 + 31, a.pq - 1) + start;
                 if (!work || i0 >= a.pq || (a.causal && j0 > qmax)) continue;
-                const bool edge = j0 + 32 > keys || i0 + 32 > a.pq || (a.causal && j0 + 31 > qmin);
-                const RaBias bias = ra_tile_bias(lut, a.reach, j0 - i0 - start - 31, j0 + 31 - qmin, j0 + l - i0 - start - 4 * g);
-                const mm_f16 s = ra_products<T, DP>(qt, 32 * u, kr, lane), dp = ra_products<T, DP>(gt, 32 * u, vr, lane);
+                const mm_f16 s = ra_products<T, R>(qt, at, kr, lane), dp = ra_products<T, R>(gt, at, vr, lane);
+                const bool far = ra_far(a.reach, j0 - i0 - start - 31, j0 + 31 - qmin);
+                const float one = lut[RA_PAD + (j0 - i0 - start - 31 >= a.reach ? 2 * a.reach : 0)];
+                const float* near = lut + (far ? 64 : j0 + l - i0 - start - 4 * g + a.reach + RA_PAD);
                 float p[16], ds[16];
+                if (far) {
 #pragma unroll
-                for (int r4 = 0; r4 < 4; ++r4) {
-                    const float* rv = rowv + 32 * u + 8 * r4 + 4 * g;
+                    for (int e = 0; e < 16; ++e) p[e] = fmaf(s[e], a.scale2, one);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) p[e] = fmaf(s[e], a.scale2, near[-((e & 3) + 8 * (e >> 2))]);
+                }
+                bool empty = false;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const float* rv = rowv + at + 8 * c + 4 * g;
                     const float4 tp = *reinterpret_cast<const float4*>(rv), ls = *reinterpret_cast<const float4*>(rv + R::BN), de = *reinterpret_cast<const float4*>(rv + 2 * R::BN);
                     const float tops[4] = {tp.x, tp.y, tp.z, tp.w}, logs[4] = {ls.x, ls.y, ls.z, ls.w}, deltas[4] = {de.x, de.y, de.z, de.w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int r = 4 * r4 + e;
-                        const float v = fmaf(s[r], a.scale2, bias.at ? bias.at[-(e + 8 * r4)] : bias.far);
-                        p[r] = exp2_fast((v - tops[e]) + logs[e]);
-                        ds[r] = p[r] * (dp[r] - deltas[e]);
-                        if (edge || logs[e] == -INFINITY) {
-                            const int i = i0 + 4 * g + e + 8 * r4;
-                            if (!mine || i >= a.pq || (a.causal && j > i + start) || logs[e] == -INFINITY) p[r] = ds[r] = 0.f;
-                        }
+                        p[4 * c + e] = exp2_fast((p[4 * c + e] - tops[e]) + logs[e]);
+                        ds[4 * c + e] = p[4 * c + e] * (dp[4 * c + e] - deltas[e]);
+                        empty |= logs[e] == -INFINITY;
                     }
                 }
-                ra_mix<T, DP>(gt, 32 * u, p, dv, lane);
-                ra_mix<T, DP>(qt, 32 * u, ds, dk, lane);
+                if (j0 + 32 > keys || i0 + 32 > a.pq || (a.causal && j0 + 31 > qmin) || ra_any(empty)) {
+                    const int from = a.causal ? j0 + l - start : 0;      // the first query that sees this key
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int ii = 4 * g + (e & 3) + 8 * (e >> 2);
+                        const bool seen = mine && i0 + ii < a.pq && i0 + ii >= from && rowv[R::BN + at + ii] != -INFINITY;
+                        p[e] = seen ? p[e] : 0.f;
+                        ds[e] = seen ? ds[e] : 0.f;
+                    }
+                }
+                ra_mix<T, R>(gt, at, p, dv, lane);
+                ra_mix<T, R>(qt, at, ds, dk, lane);
             }
         }
     }
+    ra_gather<R, WK>(dk, reinterpret_cast<float*>(ra_lds), wq, wk, lane);
+    ra_gather<R, WK>(dv, reinterpret_cast<float*>(ra_lds), wq, wk, lane);
     if (j0 + l >= a.pk) return;                            // (keys behind the last one of the sample have gradients of zero)
     T* ok = (T*)a.dk + ((int64_t)n * a.pk + j) * a.ldk + (int64_t)hk * a.d;
     T* ov = (T*)a.dv + ((int64_t)n * a.pk + j) * a.ldv + (int64_t)hk * a.d;
 #pragma unroll
-    for (int c = 0; c < R::DT; ++c)
+    for (int c = 0; c < R::DT; ++c) {
+        if (c % WK != wk) continue;
 #pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-            const int ch = 32 * c + 4 * g + 2 * r;
-            const float vk[4] = {dk[c][r] * a.scale, dk[c][r + 1] * a.scale, dk[c][r + 2] * a.scale, dk[c][r + 3] * a.scale};
-            const float vv[4] = {dv[c][r], dv[c][r + 1], dv[c][r + 2], dv[c][r + 3]};
+        for (int e = 0; e < 16; e += 4) {
+            const int ch = ra_channel(c, e, g);
+            const float vk[4] = {dk[c][e] * a.scale, dk[c][e + 1] * a.scale, dk[c][e + 2] * a.scale, dk[c][e + 3] * a.scale};
+            const float vv[4] = {dv[c][e], dv[c][e + 1], dv[c][e + 2], dv[c][e + 3]};
             if (ch < a.d) { ra_store4(ok + ch, a.d - ch, vk); ra_store4(ov + ch, a.d - ch, vv); }
         }
+    }
 }
 
 // The wavefronts' sums by distance, `lines` of them a head and sample: block (64 distances, head, share of the samples' lines) -> shares[share][head][distance]
@@ -597,54 +821,74 @@ __global__ void __launch_bounds__(RA_THREADS) relattn_buckets(const float* __res
 }
 
 static size_t ra_up(size_t b) { return (b + 255) & ~(size_t)255; }
-// Keys over several blocks where queries and heads do not fill the card twice: parts of at least 256 keys.
-static int ra_splits(const lpm_attn_geom& g, int32_t dtype) {
-    const int64_t blocks = (int64_t)g.m * g.heads * ((g.pq + RA_BM - 1) / RA_BM);
-    const int most = std::max(1, g.pk / 256);
-    if (blocks == 0 || blocks >= 512) return 1;
-    return (int)std::min<int64_t>(most, (512 + blocks - 1) / blocks);
+// Wavefronts that share rows (and walk the other side's tiles together): where blocks of 128 rows are too few to give every CU two.
+template <typename T> constexpr int ra_wide() { return sizeof(T) == 2 ? 4 : 2; }
+static bool ra_shared(int64_t blocks) { return blocks < 512; }
+static int ra_bm(int32_t dtype, int64_t pairs, int rows) {
+    return ra_shared(pairs * ((rows + 127) / 128)) ? 128 / (dtype == LPM_BF16 ? 4 : 2) : 128;
 }
-struct AttnLayout { size_t low, stats_all, part, part_ml, fwd_all, delta, diag, shares, bwd_all; };
-static AttnLayout ra_layout(const lpm_attn_geom& g, int32_t dtype, int splits) {
+// The forward pass's blocks: rows folded over the heads that share keys where these fit two operands of 32 rows, and the keys over several blocks where they
+// are long and the blocks do not fill the card.
+struct RaForward { bool fold; int bm, splits; };
+static RaForward ra_plan(const lpm_attn_geom& g, int32_t dtype) {
+    RaForward f{};
+    const int share = g.heads / g.kv_heads;
+    f.fold = share > 1 && g.pq <= 32 && share * g.pq <= 64 && share * ra_lut(g.reach) <= 8192;
+    const int rows = f.fold ? share * g.pq : g.pq;
+    const int64_t pairs = (int64_t)g.m * (f.fold ? g.kv_heads : g.heads);
+    f.bm = ra_bm(dtype, pairs, rows);
+    const int64_t blocks = std::max<int64_t>(1, pairs * ((rows + f.bm - 1) / f.bm));
+    f.splits = blocks >= 512 ? 1 : (int)std::min<int64_t>({std::max(1, g.pk / 512), (1024 + blocks - 1) / blocks, RA_MAX_SPLITS});
+    return f;
+}
+struct AttnLayout { size_t part_ml, fwd_all, diag, shares, bwd_all; int lines; };
+static AttnLayout ra_layout(const lpm_attn_geom& g, int32_t dtype) {
     AttnLayout o;
-    const size_t rows = (size_t)g.m * g.heads * g.pq, nd = 2 * (size_t)g.reach + 1;
-    o.low = ra_up(rows * 8);
-    o.stats_all = o.low + (dtype == LPM_BF16 ? ra_up(rows * g.d * 2) : 0);
-    o.part = 0;
-    o.part_ml = splits > 1 ? ra_up((size_t)splits * rows * g.d * 4) : 0;
-    o.fwd_all = splits > 1 ? o.part_ml + ra_up((size_t)splits * rows * 8) : 0;
-    o.delta = 0;
+    const RaForward f = ra_plan(g, dtype);
+    const size_t rows = (size_t)g.m * g.heads * g.pq, nd = ra_distances(g.reach);
+    const int bm = ra_bm(dtype, (int64_t)g.m * g.heads, g.pq);
+    o.lines = (g.pq + bm - 1) / bm * RA_WAVES;
+    o.part_ml = f.splits > 1 ? ra_up((size_t)f.splits * rows * g.d * 4) : 0;
+    o.fwd_all = f.splits > 1 ? o.part_ml + ra_up((size_t)f.splits * rows * 8) : 0;
     o.diag = ra_up(rows * 4);
-    o.shares = o.diag + (g.n_buckets ? ra_up((size_t)g.m * g.heads * ((g.pq + 31) / 32) * nd * 4) : 0);
+    o.shares = o.diag + (g.n_buckets ? ra_up((size_t)g.m * g.heads * o.lines * nd * 4) : 0);
     o.bwd_all = o.shares + (g.n_buckets ? ra_up((size_t)RA_SHARES * g.heads * nd * 4) : 0);
     return o;
 }
 
-template <typename T, int DP, bool KEEP> static hipError_t ra_forward(const AttnArgs& a, hipStream_t st) {
-    typedef Ra<T, DP> R;
+template <typename K> static hipError_t ra_launch(K kernel, DeviceSet& done, int64_t blocks, size_t lds, const AttnArgs& a, hipStream_t st) {
+    if (!blocks) return hipSuccess;
+    const hipError_t e = allow_lds(kernel, 160 * 1024, done);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(RA_THREADS), lds, st, a);
+    return hipGetLastError();
+}
+template <typename T, int DP, int WK> static hipError_t ra_forward(const AttnArgs& a, hipStream_t st) {
+    typedef Ra<T, DP, WK> R;
     static DeviceSet done;
-    const size_t lds = 2 * R::TILE + (2 * (size_t)a.reach + 1 + 2 * RA_PAD) * 4;
-    const hipError_t e = allow_lds(relattn_fwd<T, DP, KEEP>, 160 * 1024 - 256, done);
-    if (e != hipSuccess) return e;
-    const int tiles = (a.pq + RA_BM - 1) / RA_BM;
-    hipLaunchKernelGGL((relattn_fwd<T, DP, KEEP>), dim3((unsigned)(a.m * a.H * tiles * a.splits)), dim3(RA_THREADS), lds, st, a);
-    return hipGetLastError();
+    const int share = a.H / a.G, rows = a.fold ? share * a.pq : a.pq;
+    return ra_launch(relattn_fwd<T, DP, WK>, done, (int64_t)a.m * (a.fold ? a.G : a.H) * ((rows + R::BM - 1) / R::BM) * a.splits,
+                     2 * R::TILE + (size_t)(a.fold ? share : 1) * ra_lut(a.reach) * 4, a, st);
 }
-template <typename T, int DP> static hipError_t ra_backward(const AttnArgs& a, hipStream_t st) {
-    typedef Ra<T, DP> R;
-    static DeviceSet done_q, done_kv;
-    const size_t lut = (2 * (size_t)a.reach + 1 + 2 * RA_PAD) * 4;
-    hipError_t e = allow_lds(relattn_bwd_q<T, DP>, 160 * 1024 - 256, done_q);
-    if (e == hipSuccess) e = allow_lds(relattn_bwd_kv<T, DP>, 160 * 1024 - 256, done_kv);
-    if (e != hipSuccess) return e;
-    const int qt = (a.pq + RA_BM - 1) / RA_BM, kt = (a.pk + RA_BM - 1) / RA_BM;
-    if (qt) hipLaunchKernelGGL((relattn_bwd_q<T, DP>), dim3((unsigned)(a.m * a.H * qt)), dim3(RA_THREADS), 2 * R::TILE + RA_WAVES * 63 * RA_DIAG_PITCH * 4 + lut, st, a);
-    if (kt) hipLaunchKernelGGL((relattn_bwd_kv<T, DP>), dim3((unsigned)(a.m * a.G * kt)), dim3(RA_THREADS), 2 * R::TILE + 3 * R::BN * 4 + lut, st, a);
-    return hipGetLastError();
+template <typename T, int DP, int WK> static hipError_t ra_backward_q(const AttnArgs& a, hipStream_t st) {
+    typedef Ra<T, DP, WK> R;
+    static DeviceSet done;
+    static_assert(2 * R::TILE + RA_WAVES * 63 * RA_DIAG_PITCH * 4 + (2 * RA_MAX_REACH + 1 + 2 * RA_PAD) * 4 <= 160 * 1024, "the tiles, diagonals and bias fit");
+    static_assert(WK == 1 || 128 / WK / 32 * WK * R::DT * 4096 <= 2 * R::TILE, "the sums of wavefronts that share rows fit over the tiles");
+    return ra_launch(relattn_bwd_q<T, DP, WK>, done, (int64_t)a.m * a.H * ((a.pq + R::BM - 1) / R::BM),
+                     2 * R::TILE + RA_WAVES * 63 * RA_DIAG_PITCH * 4 + (size_t)ra_lut(a.reach) * 4, a, st);
 }
-#define LPM_RA(dtype_, d_, call_)                                                          \
-    ((dtype_) == LPM_BF16 ? ((d_) <= 32 ? call_(bf16_t, 32) : (d_) <= 64 ? call_(bf16_t, 64) : (d_) <= 96 ? call_(bf16_t, 96) : call_(bf16_t, 128)) \
-                          : ((d_) <= 32 ? call_(float, 32) : (d_) <= 64 ? call_(float, 64) : (d_) <= 96 ? call_(float, 96) : call_(float, 128)))
+template <typename T, int DP, int WK> static hipError_t ra_backward_kv(const AttnArgs& a, hipStream_t st) {
+    typedef Ra<T, DP, WK> R;
+    static DeviceSet done;
+    return ra_launch(relattn_bwd_kv<T, DP, WK>, done, (int64_t)a.m * a.G * ((a.pk + R::BM - 1) / R::BM), 2 * R::TILE + (3 * R::BN + (size_t)ra_lut(a.reach)) * 4, a, st);
+}
+// f<T, padded channels, wavefronts that share rows>
+#define LPM_RA_WIDE(f_, T_, DP_, shared_) ((shared_) ? f_<T_, DP_, ra_wide<T_>()>(a, st) : f_<T_, DP_, 1>(a, st))
+#define LPM_RA_CHANNELS(f_, T_, shared_)                                                                                   \
+    (a.d <= 32 ? LPM_RA_WIDE(f_, T_, 32, shared_) : a.d <= 64 ? LPM_RA_WIDE(f_, T_, 64, shared_)                          \
+     : a.d <= 96 ? LPM_RA_WIDE(f_, T_, 96, shared_) : LPM_RA_WIDE(f_, T_, 128, shared_))
+#define LPM_RA(f_, dtype_, shared_) ((dtype_) == LPM_BF16 ? LPM_RA_CHANNELS(f_, bf16_t, shared_) : LPM_RA_CHANNELS(f_, float, shared_))
 
 }  // namespace lpm
 
@@ -659,16 +903,17 @@ static int32_t ra_check(const lpm_attn_geom* g, int32_t dtype, lpm_attn_geom& o)
         return fail(LPM_ESHAPE, "%d buckets (0 to 65536) of distances up to %d (0 to %d)", o.n_buckets, o.reach, RA_MAX_REACH);
     if (!(o.scale >= 0.f) || o.scale > 1e30f) return fail(LPM_EINVAL, "scale must be a number of 0 (for 1 / sqrt(d)) or more");
     const int64_t wq = (int64_t)o.heads * o.d, wk = (int64_t)o.kv_heads * o.d;
-    if (wq >= (1 << 28)) return fail(LPM_ESHAPE, "%d heads of %d channels", o.heads, o.d);
+    if (wq > RA_MAX_LD) return fail(LPM_ESHAPE, "%d heads of %d channels", o.heads, o.d);
     if (!o.ldq) o.ldq = (int32_t)wq;
     if (!o.ldk) o.ldk = (int32_t)wk;
     if (!o.ldv) o.ldv = (int32_t)wk;
     if (!o.ldy) o.ldy = (int32_t)wq;
     if (o.ldq < wq || o.ldy < wq || o.ldk < wk || o.ldv < wk) return fail(LPM_ESHAPE, "positions closer than their heads are wide");
+    if (std::max({o.ldq, o.ldk, o.ldv, o.ldy}) > RA_MAX_LD) return fail(LPM_ESHAPE, "positions more than %d elements apart", RA_MAX_LD);
     if (o.scale == 0.f) o.scale = 1.f / sqrtf((float)o.d);
     if (!o.n_buckets) o.reach = 0;
     const int64_t most = std::max<int64_t>(o.pq, o.pk) / 32 + 1;
-    if ((int64_t)o.m * o.heads > (int64_t)1 << 31 || (int64_t)o.m * o.heads * most >= (int64_t)1 << 31) return fail(LPM_ESHAPE, "more blocks than a launch takes");
+    if ((int64_t)o.m * o.heads >= ((int64_t)1 << 31) / most / RA_MAX_SPLITS) return fail(LPM_ESHAPE, "more blocks than a launch takes");
     return LPM_OK;
 }
 static AttnArgs ra_args(const lpm_attn_geom& g, const void* q, const void* k, const void* v, const int32_t* len, const int32_t* start, const int32_t* map,
@@ -698,7 +943,7 @@ extern "C" int32_t lpm_attn_ws_bytes(const lpm_attn_geom* geom, int32_t dtype, s
     lpm_attn_geom g;
     const int32_t rc = ra_check(geom, dtype, g);
     if (rc) return rc;
-    const AttnLayout o = ra_layout(g, dtype, ra_splits(g, dtype));
+    const AttnLayout o = ra_layout(g, dtype);
     if (forward) *forward = o.fwd_all;
     if (backward) *backward = o.bwd_all;
     return LPM_OK;
@@ -709,7 +954,7 @@ extern "C" int32_t lpm_attn_stats_bytes(const lpm_attn_geom* geom, int32_t dtype
     lpm_attn_geom g;
     const int32_t rc = ra_check(geom, dtype, g);
     if (rc) return rc;
-    *bytes = ra_layout(g, dtype, 1).stats_all;
+    *bytes = (size_t)g.m * g.heads * g.pq * sizeof(float2_);
     return LPM_OK;
 }
 
@@ -722,18 +967,16 @@ extern "C" int32_t lpm_attn_forward(const lpm_attn_geom* geom, int32_t dtype, co
     if (g.m == 0 || g.pq == 0) return LPM_OK;
     if (!q || !y || (g.pk > 0 && (!k || !v))) return fail(LPM_EINVAL, "NULL argument");
     AttnArgs a = ra_args(g, q, k, v, key_len, q_start, map, table);
-    a.splits = ra_splits(g, dtype);
+    const RaForward plan = ra_plan(g, dtype);
+    a.splits = plan.splits;
+    a.fold = plan.fold;
     if (a.splits > 1 && !ws) return fail(LPM_EINVAL, "scratch required");
-    const AttnLayout o = ra_layout(g, dtype, a.splits);
     a.y = y;
     a.stats = (float2_*)stats;
-    a.low = stats && dtype == LPM_BF16 ? (bf16_t*)((char*)stats + o.low) : nullptr;
     a.part = (float*)ws;
-    a.part_ml = (float*)((char*)ws + o.part_ml);
+    a.part_ml = (float*)((char*)ws + ra_layout(g, dtype).part_ml);
     hipStream_t st = (hipStream_t)stream;
-#define LPM_RA_CALL(T_, DP_) (stats ? ra_forward<T_, DP_, true>(a, st) : ra_forward<T_, DP_, false>(a, st))
-    LPM_HIP(LPM_RA(dtype, g.d, LPM_RA_CALL));
-#undef LPM_RA_CALL
+    LPM_HIP(LPM_RA(ra_forward, dtype, plan.bm < 128));
     if (a.splits > 1) {
         const dim3 grid((unsigned)(((int64_t)g.m * g.heads * g.pq + RA_WAVES - 1) / RA_WAVES));
         if (dtype == LPM_BF16) hipLaunchKernelGGL(relattn_join<bf16_t>, grid, dim3(RA_THREADS), 0, st, a);
@@ -754,26 +997,22 @@ extern "C" int32_t lpm_attn_backward(const lpm_attn_geom* geom, int32_t dtype, c
     const bool queries = g.m > 0 && g.pq > 0, keys = g.m > 0 && g.pk > 0;
     if ((queries && (!q || !y || !stats || !dy || !dq)) || (keys && (!k || !v || !dk || !dv))) return fail(LPM_EINVAL, "NULL argument");
     if ((queries || dtable) && !ws) return fail(LPM_EINVAL, "scratch required");
-    const AttnLayout o = ra_layout(g, dtype, 1);
+    const AttnLayout o = ra_layout(g, dtype);
     AttnArgs a = ra_args(g, q, k, v, key_len, q_start, map, table);
     a.y = const_cast<void*>(y);
     a.dy = dy;
     a.dq = dq; a.dk = dk; a.dv = dv;
     a.stats = (float2_*)const_cast<void*>(stats);
-    a.low = dtype == LPM_BF16 && stats ? (bf16_t*)((char*)const_cast<void*>(stats) + o.low) : nullptr;
     a.delta = (float*)ws;
     a.diag = dtable ? (float*)((char*)ws + o.diag) : nullptr;
     hipStream_t st = (hipStream_t)stream;
-    if (queries || keys) {
-#define LPM_RA_CALL(T_, DP_) ra_backward<T_, DP_>(a, st)
-        LPM_HIP(LPM_RA(dtype, g.d, LPM_RA_CALL));
-#undef LPM_RA_CALL
-    }
+    if (queries) LPM_HIP(LPM_RA(ra_backward_q, dtype, ra_bm(dtype, (int64_t)g.m * g.heads, g.pq) < 128));
+    if (keys) LPM_HIP(LPM_RA(ra_backward_kv, dtype, ra_bm(dtype, (int64_t)g.m * g.kv_heads, g.pk) < 128));
     if (dtable) {
-        const int nd = 2 * g.reach + 1, lines = (g.pq + 31) / 32;
+        const int nd = 2 * g.reach + 1;
         float* shares = (float*)((char*)ws + o.shares);
         hipLaunchKernelGGL(relattn_diagonals, dim3((unsigned)((nd + 63) / 64), (unsigned)g.heads, RA_SHARES), dim3(RA_THREADS), 0, st, (const float*)a.diag, g.m,
-                           g.heads, lines, nd, shares);
+                           g.heads, o.lines, nd, shares);
         hipLaunchKernelGGL(relattn_buckets, dim3((unsigned)g.heads), dim3(RA_THREADS), (size_t)nd * 4, st, (const float*)shares, map, g.heads, g.n_buckets, nd, dtable,
                            accumulate);
         LPM_HIP(hipGetLastError());
