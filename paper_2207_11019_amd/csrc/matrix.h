@@ -39,11 +39,13 @@ template <> struct Mm<bf16_t> {
         return make_uint2(e[0] | e[1] << 16, e[2] | e[3] << 16);
 #endif
     }
-    // operand whose rows are the columns col .. col + 31 of a tile in LDS and whose terms are its rows, in the order in which a result lies over
-    // the lanes: those of half g are row + 4 g + (0 .. 3) and row + 8 + 4 g + (0 .. 3)
-    static __device__ __forceinline__ uint4 columns(const unsigned char* tile, int pitch, int row, int col, int lane) {
-        const unsigned char* p = tile + (row + 4 * (lane >> 5) + ((lane >> 2) & 3)) * pitch + (col + (lane & 16) + 4 * (lane & 3)) * 2;
-        const uint2 a = read4(p), b = read4(p + 8 * pitch);
+    // Operand whose rows are the channels 32 t .. 32 t + 31 of a tile's rows in LDS (R: bytes of a row, and where a row's chunks lie) and whose terms are its
+    // rows, in the order in which a result lies over the lanes: those of half g are 4 g + (0 .. 3) and 8 + 4 g + (0 .. 3); place() does not
+    // differ between rows 8 apart
+    template <typename R> static __device__ __forceinline__ uint4 columns(const unsigned char* tile, int t, int lane) {
+        const int row = 4 * (lane >> 5) + ((lane >> 2) & 3);
+        const unsigned char* p = tile + row * R::ROW + (((4 * t + ((lane >> 3) & 2) + ((lane >> 1) & 1)) ^ R::place(row)) * 16 + (lane & 1) * 8);
+        const uint2 a = read4(p), b = read4(p + 8 * R::ROW);
         return make_uint4(a.x, a.y, b.x, b.y);
     }
 };
@@ -58,10 +60,15 @@ template <> struct Mm<float> {
     static __device__ __forceinline__ uint4 pack(const float* v) {
         return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
     }
-    // ... the rows of half g: row + 4 g + (0 .. 3)
-    static __device__ __forceinline__ uint4 columns(const unsigned char* tile, int pitch, int row, int col, int lane) {
-        const unsigned char* p = tile + (row + 4 * (lane >> 5)) * pitch + (col + (lane & 31)) * 4;
-        return make_uint4(*(const unsigned*)p, *(const unsigned*)(p + pitch), *(const unsigned*)(p + 2 * pitch), *(const unsigned*)(p + 3 * pitch));
+    // ... the rows of half g: 4 g + (0 .. 3)
+    template <typename R> static __device__ __forceinline__ uint4 columns(const unsigned char* tile, int t, int lane) {
+        unsigned v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int row = 4 * (lane >> 5) + k;
+            v[k] = *reinterpret_cast<const unsigned*>(tile + row * R::ROW + (((8 * t + ((lane & 31) >> 2)) ^ R::place(row)) * 16 + (lane & 3) * 4));
+        }
+        return make_uint4(v[0], v[1], v[2], v[3]);
     }
 };
 
@@ -72,18 +79,6 @@ __device__ __forceinline__ float exp2_fast(float x) {
 #else
     return exp2f(x);
 #endif
-}
-
-// the first n of the EPC elements at p (an element's alignment is enough), zeros beyond; n may be negative or larger
-template <typename T> __device__ __forceinline__ uint4 ld16(const T* p, int n) {
-    constexpr int EPC = Mm<T>::EPC;
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (n >= EPC) { __builtin_memcpy(&v, p, 16); return v; }
-    T e[EPC] = {};
-#pragma unroll
-    for (int k = 0; k < EPC; ++k) if (k < n) e[k] = p[k];
-    __builtin_memcpy(&v, e, 16);
-    return v;
 }
 
 }  // namespace lpm

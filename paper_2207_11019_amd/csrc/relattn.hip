@@ -11,6 +11,7 @@
 // reach add one number.  Its gradient: sums of ds along the diagonals of 32 x 32 tiles, which a wavefront carries from tile to tile, so that each
 // distance is stored once per wavefront; two small kernels add up wavefronts, then the distances of a bucket.  No atomics: every sum has one order.
 #include "matrix.h"
+#include "lds_dma.h"
 #include "lpm_internal.h"
 #include <algorithm>
 #include <cmath>
@@ -44,16 +45,23 @@ struct AttnArgs {
     float *delta, *diag;                  // backward: [row], [m H][lines][2 reach + 1]
 };
 
-// WK wavefronts share a block's 128 / WK rows, each with its 32 rows of every tile of the other side
-template <typename T, int DP, int WK> struct Ra {
+// WK wavefronts share a block's 128 / WK rows, each with its 32 rows of every tile of the other side.  DMA: tiles go straight from memory to LDS (channels in
+// whole 16-byte chunks, rows on whole dwords); else by way of registers, where a row's last chunk is put in order.
+template <typename T, int DP, int WK_, bool DMA_> struct Ra {
+    static constexpr int WK = WK_;
+    static constexpr bool DMA = DMA_;
     static constexpr int EPC = Mm<T>::EPC, CHUNKS = DP / EPC, KS = DP / (2 * EPC), ES = (int)sizeof(T);
     static constexpr int BM = 128 / WK;
     static constexpr int BN = WK > 1 ? 32 * WK : ES == 2 ? 64 : 32;      // rows of a staged tile
     static constexpr int SUB = BN / (32 * WK);                // 32-row pieces of it that a wavefront takes
-    static constexpr int PITCH = DP * ES + 32;                // rows 8 dwords apart in the banks: row-wise and column-wise reads are free of conflicts
-    static constexpr int TILE = BN * PITCH;
+    static constexpr int ROW = DP * ES;                       // bytes
+    static constexpr int TILE = BN * ROW;
+    static constexpr int STAGES = 2;
+    static constexpr int LDS = 2 * STAGES * TILE;             // tiles of both operands
     static constexpr int PER = BN * CHUNKS / RA_THREADS;      // chunks of a tile a thread brings
     static constexpr int DT = DP / 32;                        // 32-channel pieces of a head
+    // Chunk c of a row lies at position c ^ place(row): eight consecutive rows at one chunk, and four at two neighbouring ones, are on distinct banks.
+    static __device__ __forceinline__ int place(int row) { return (ROW % 256 == 0 ? row & 7 : ROW % 128 == 0 ? (row >> 1) & 3 : (row >> 2) & 1) << 1; }
 };
 
 // Sixteen bytes of a row of d channels from channel c on, through a buffer whose end is the last row's: rows beyond are zeros.  Where d is no whole
@@ -61,67 +69,71 @@ template <typename T, int DP, int WK> struct Ra {
 template <typename T> __device__ __forceinline__ unsigned ra_offset(int64_t row, int64_t ld, int c, int d) {
     constexpr int EPC = Mm<T>::EPC;
     if (c >= d) return 0xffffffffu;
-    return (unsigned)((row * ld + (c + EPC > d ? (d > EPC ? d - EPC : 0) : c)) * (int64_t)sizeof(T));
+    return (unsigned)((row * ld + (c + EPC > d ? d - EPC : c)) * (int64_t)sizeof(T));
+}
+template <typename T> __device__ __forceinline__ unsigned ra_bytes(int64_t ld, int rows, int d) {
+    return rows > 0 ? (unsigned)(((int64_t)(rows - 1) * ld + d) * (int64_t)sizeof(T)) : 0u;
 }
 template <typename T> __device__ __forceinline__ __amdgpu_buffer_rsrc_t ra_buffer(const T* base, int64_t ld, int rows, int d) {
-    const unsigned bytes = rows > 0 ? (unsigned)(((int64_t)(rows - 1) * ld + d) * (int64_t)sizeof(T)) : 0u;
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, bytes, 0x00020000);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, ra_bytes<T>(ld, rows, d), 0x00020000);
 }
 typedef unsigned int ra_u4 __attribute__((ext_vector_type(4)));
-template <typename T> __device__ __forceinline__ uint4 ra_load(__amdgpu_buffer_rsrc_t r, unsigned off, int d) {
-    constexpr int EPC = Mm<T>::EPC;
-    if (d >= EPC) {
-        const ra_u4 v = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
-        return make_uint4(v.x, v.y, v.z, v.w);
-    }
-    unsigned e[4] = {0, 0, 0, 0};          // heads narrower than a chunk, element by element
-#pragma unroll
-    for (int k = 0; k < EPC; ++k) {
-        if (k >= d) break;
-        const unsigned o = off == 0xffffffffu ? off : off + k * (unsigned)sizeof(T);
-        if (sizeof(T) == 2) e[k >> 1] |= (unsigned)(unsigned short)__builtin_amdgcn_raw_buffer_load_b16(r, o, 0, 0) << (16 * (k & 1));
-        else e[k] = __builtin_amdgcn_raw_buffer_load_b32(r, o, 0, 0);
-    }
-    return make_uint4(e[0], e[1], e[2], e[3]);
+__device__ __forceinline__ uint4 ra_load(__amdgpu_buffer_rsrc_t r, unsigned off) {
+    const ra_u4 v = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
+    return make_uint4(v.x, v.y, v.z, v.w);
 }
 template <typename T> __device__ __forceinline__ uint4 ra_shift(uint4 v, int c, int d) {
     constexpr int EPC = Mm<T>::EPC;
-    const int s = c + EPC > d && c < d && d > EPC ? (c + EPC - d) * 8 * (int)sizeof(T) : 0;
+    const int s = c + EPC > d && c < d ? (c + EPC - d) * 8 * (int)sizeof(T) : 0;
     uint64_t lo = v.x | (uint64_t)v.y << 32, hi = v.z | (uint64_t)v.w << 32;
     lo = s >= 64 ? hi >> (s & 63) : s ? lo >> s | hi << (64 - s) : lo;
     hi = s >= 64 ? 0 : hi >> s;
     return make_uint4((unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32));
 }
 
-// A tile on its way from memory to LDS, in registers meanwhile
+// A tile on its way from memory to LDS, straight or in registers meanwhile: load() into stage `s` of the operand's ring, done() before the barrier behind
+// which the tile is read.  The stage that load() writes is one that no wavefront reads any more: its tile was the one before the last barrier's.
 template <typename T, typename R> struct RaTile {
-    uint4 v[R::PER];
+    uint4 v[R::DMA ? 1 : R::PER];
     unsigned off[R::PER];
-    __device__ __forceinline__ void place(int64_t ld, int d) {
+    unsigned char* lds;
+    __device__ __forceinline__ void place(unsigned char* ring, int64_t ld, int d) {
+        lds = ring;
 #pragma unroll
         for (int i = 0; i < R::PER; ++i) {
             const int at = i * RA_THREADS + (int)threadIdx.x, r = at / R::CHUNKS;
-            off[i] = ra_offset<T>(r, ld, (at - r * R::CHUNKS) * R::EPC, d);
+            off[i] = ra_offset<T>(r, ld, ((at - r * R::CHUNKS) ^ R::place(r)) * R::EPC, d);
         }
     }
     // rows row0 .. of `rows`
-    __device__ __forceinline__ void load(const T* base, int64_t ld, int row0, int rows, int d) {
-        const auto buf = ra_buffer(base + (int64_t)row0 * ld, ld, min(rows - row0, R::BN), d);
+    __device__ __forceinline__ void load(const T* base, int64_t ld, int row0, int rows, int d, int s) {
+        const int n = min(rows - row0, R::BN);
+        base += (int64_t)row0 * ld;
+        if constexpr (R::DMA) {
+            const u32x4_ buf = buffer_words(base, ra_bytes<T>(ld, n, d));
+            unsigned char* to = lds + s * 2 * R::TILE + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 1024;
 #pragma unroll
-        for (int i = 0; i < R::PER; ++i) v[i] = ra_load<T>(buf, off[i], d);
-    }
-    __device__ __forceinline__ void store(unsigned char* lds, int d) {
-        if (d % R::EPC) {
+            for (int i = 0; i < R::PER; ++i) load_to_lds16(buf, to + i * RA_THREADS * 16, off[i]);
+        } else {
+            const auto buf = ra_buffer(base, ld, n, d);
 #pragma unroll
-            for (int i = 0; i < R::PER; ++i) v[i] = ra_shift<T>(v[i], (i * RA_THREADS + (int)threadIdx.x) % R::CHUNKS * R::EPC, d);
+            for (int i = 0; i < R::PER; ++i) v[i] = ra_load(buf, off[i]);
         }
+    }
+    __device__ __forceinline__ void done(int d, int s) {
+        if constexpr (!R::DMA) {
 #pragma unroll
-        for (int i = 0; i < R::PER; ++i) {
-            const int at = i * RA_THREADS + (int)threadIdx.x, r = at / R::CHUNKS, c = at - r * R::CHUNKS;
-            *reinterpret_cast<uint4*>(lds + r * R::PITCH + c * 16) = v[i];
+            for (int i = 0; i < R::PER; ++i) {
+                const int at = i * RA_THREADS + (int)threadIdx.x, r = at / R::CHUNKS;
+                const uint4 w = d % R::EPC ? ra_shift<T>(v[i], ((at - r * R::CHUNKS) ^ R::place(r)) * R::EPC, d) : v[i];
+                *reinterpret_cast<uint4*>(lds + s * 2 * R::TILE + at * 16) = w;
+            }
         }
     }
 };
+template <typename R> __device__ __forceinline__ void ra_landed() {
+    if constexpr (R::DMA) LPM_WAIT_VM(0);
+}
 // a wavefront's 32 rows as an operand: the lane's row (below `rows`, or zeros), its half of every 2 * EPC channels
 template <typename T, typename R> struct RaRows {
     uint4 v[R::KS];
@@ -130,11 +142,11 @@ template <typename T, typename R> struct RaRows {
 #pragma unroll
         for (int s = 0; s < R::KS; ++s) {
             const int c = (2 * s + g) * R::EPC;
-            v[s] = ra_load<T>(buf, there ? ra_offset<T>(row, ld, c, d) : 0xffffffffu, d);
+            v[s] = ra_load(buf, there ? ra_offset<T>(row, ld, c, d) : 0xffffffffu);
         }
-        if (d % R::EPC) {
+        if constexpr (!R::DMA) {
 #pragma unroll
-            for (int s = 0; s < R::KS; ++s) v[s] = ra_shift<T>(v[s], (2 * s + g) * R::EPC, d);
+            for (int s = 0; s < R::KS; ++s) if (d % R::EPC) v[s] = ra_shift<T>(v[s], (2 * s + g) * R::EPC, d);
         }
     }
 };
@@ -142,9 +154,10 @@ template <typename T, typename R> struct RaRows {
 template <typename T, typename R>
 __device__ __forceinline__ mm_f16 ra_products(const unsigned char* tile, int row, const RaRows<T, R>& own, int lane) {
     mm_f16 acc = {};
-    const unsigned char* p = tile + (row + (lane & 31)) * R::PITCH + (lane >> 5) * 16;
+    const unsigned char* p = tile + (row + (lane & 31)) * R::ROW;
+    const int at = (lane >> 5) ^ R::place(lane & 31);
 #pragma unroll
-    for (int s = 0; s < R::KS; ++s) acc = Mm<T>::mul(*reinterpret_cast<const uint4*>(p + s * 32), own.v[s], acc);
+    for (int s = 0; s < R::KS; ++s) acc = Mm<T>::mul(*reinterpret_cast<const uint4*>(p + (at ^ (2 * s)) * 16), own.v[s], acc);
     return acc;
 }
 // out[t][channel 32 t + .][own row] += sum over the tile's rows row .. row + 31 of tile[row][channel] w[row][own row], w as a result lies
@@ -154,16 +167,16 @@ __device__ __forceinline__ void ra_mix(const unsigned char* tile, int row, const
     for (int u = 0; u < 16 / R::EPC; ++u) {
         const uint4 b = Mm<T>::pack(w + u * R::EPC);
 #pragma unroll
-        for (int t = 0; t < R::DT; ++t) out[t] = Mm<T>::mul(Mm<T>::columns(tile, R::PITCH, row + 2 * R::EPC * u, 32 * t, lane), b, out[t]);
+        for (int t = 0; t < R::DT; ++t) out[t] = Mm<T>::mul(Mm<T>::template columns<R>(tile + (row + 2 * R::EPC * u) * R::ROW, t, lane), b, out[t]);
     }
 }
-// four consecutive channels of a row
-template <typename T>
+// four consecutive channels of a row, n of them there (WHOLE: all)
+template <bool WHOLE, typename T>
 __device__ __forceinline__ void ra_store4(T* p, int n, const float (&v)[4]) {
     T e[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) e[k] = to_store<T>(v[k]);
-    if (n >= 4) { __builtin_memcpy(p, e, 4 * sizeof(T)); return; }
+    if (WHOLE || n >= 4) { __builtin_memcpy(p, e, 4 * sizeof(T)); return; }
 #pragma unroll
     for (int k = 0; k < 4; ++k) if (k < n) p[k] = e[k];
 }
@@ -172,8 +185,9 @@ __device__ __forceinline__ int ra_channel(int t, int r, int g) { return 32 * t +
 
 // Sums over the WK wavefronts that share rows, by pieces of 32 channels: afterwards wavefront wk holds the sums of the pieces t with t % WK == wk.  `area`
 // is no longer read by anybody; every wavefront calls.
-template <typename R, int WK>
+template <typename R>
 __device__ __forceinline__ void ra_gather(mm_f16 (&out)[R::DT], float* area, int wq, int wk, int lane) {
+    constexpr int WK = R::WK;
     if (WK == 1) return;
     float* mine = area + (int64_t)(wq * WK) * R::DT * 1024;
     __syncthreads();
@@ -247,12 +261,11 @@ __device__ __forceinline__ RaBlock ra_block(int heads, int tiles, int splits) {
     return r;
 }
 
-template <typename T, int DP, int WK>
+template <typename T, int DP, int WK, bool DMA>
 __global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
-    typedef Ra<T, DP, WK> R;
+    typedef Ra<T, DP, WK, DMA> R;
     extern __shared__ __attribute__((aligned(16))) unsigned char ra_lds[];
-    unsigned char *kt = ra_lds, *vt = ra_lds + R::TILE;
-    float* lut = reinterpret_cast<float*>(ra_lds + 2 * R::TILE);
+    float* lut = reinterpret_cast<float*>(ra_lds + R::LDS);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 31, g = lane >> 5, wq = wave / WK, wk = wave % WK;
     const int share = a.H / a.G, rows = a.fold ? share * a.pq : a.pq, tiles = (rows + R::BM - 1) / R::BM;
     RaBlock b = ra_block(a.fold ? a.G : a.H, tiles, a.splits);
@@ -269,9 +282,9 @@ __global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
     if (a.causal) end = ra_clamp((a.fold ? a.pq : min(b.tile * R::BM + R::BM, a.pq)) + start, 0, keys);
     const int all = (end + R::BN - 1) / R::BN, per = (all + a.splits - 1) / a.splits, t0 = b.split * per, t1 = min(all, t0 + per);
     RaTile<T, R> kr, vr;
-    kr.place(a.ldk, a.d);
-    vr.place(a.ldv, a.d);
-    if (t0 < t1) { kr.load(kb, a.ldk, t0 * R::BN, end, a.d); vr.load(vb, a.ldv, t0 * R::BN, end, a.d); }
+    kr.place(ra_lds, a.ldk, a.d);
+    vr.place(ra_lds + R::TILE, a.ldv, a.d);
+    if (t0 < t1) { kr.load(kb, a.ldk, t0 * R::BN, end, a.d, t0 & 1); vr.load(vb, a.ldv, t0 * R::BN, end, a.d, t0 & 1); }
     RaRows<T, R> qr;
     if (a.fold)                             // (rows of other heads lie d elements apart: from the sample's first query on)
         qr.load((const T*)a.q + ((int64_t)n * a.pq + i) * a.ldq + (int64_t)h * a.d, 0, 0, work, 1, a.d, g);
@@ -282,11 +295,12 @@ __global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
     mm_f16 o[R::DT] = {};
     float top = -INFINITY, sum = 0.f;
     for (int t = t0; t < t1; ++t) {
+        const unsigned char *kt = ra_lds + (t & 1) * 2 * R::TILE, *vt = kt + R::TILE;
+        kr.done(a.d, t & 1);
+        vr.done(a.d, t & 1);
+        ra_landed<R>();
         __syncthreads();
-        kr.store(kt, a.d);
-        vr.store(vt, a.d);
-        __syncthreads();
-        if (t + 1 < t1) { kr.load(kb, a.ldk, (t + 1) * R::BN, end, a.d); vr.load(vb, a.ldv, (t + 1) * R::BN, end, a.d); }
+        if (t + 1 < t1) { kr.load(kb, a.ldk, (t + 1) * R::BN, end, a.d, (t + 1) & 1); vr.load(vb, a.ldv, (t + 1) * R::BN, end, a.d, (t + 1) & 1); }
         const int j0 = t * R::BN + wk * 32 * R::SUB;       // the wavefront's keys of the tile
         if (!work || j0 >= end || (a.causal && j0 > qmax)) continue;
         const int last = j0 + 32 * R::SUB - 1;
@@ -366,7 +380,7 @@ __global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
             for (int e = 0; e < 16; ++e) o[c][e] *= shrink;
         top = to;
         sum = all_sum;
-        ra_gather<R, WK>(o, reinterpret_cast<float*>(ra_lds), wq, wk, lane);
+        ra_gather<R>(o, reinterpret_cast<float*>(ra_lds), wq, wk, lane);
     }
     if (r0 + l >= rows) return;
     const int64_t row = ((int64_t)n * a.H + h) * a.pq + i;
@@ -380,7 +394,7 @@ __global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
             for (int e = 0; e < 16; e += 4) {
                 const int ch = ra_channel(c, e, g);
                 const float v[4] = {o[c][e], o[c][e + 1], o[c][e + 2], o[c][e + 3]};
-                if (ch < a.d) ra_store4(a.part + at * a.d + ch, a.d - ch, v);
+                if (ch < a.d) ra_store4<R::DMA>(a.part + at * a.d + ch, a.d - ch, v);
             }
         }
         return;
@@ -395,7 +409,7 @@ __global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
         for (int e = 0; e < 16; e += 4) {
             const int ch = ra_channel(c, e, g);
             const float v[4] = {o[c][e] * inv, o[c][e + 1] * inv, o[c][e + 2] * inv, o[c][e + 3] * inv};
-            if (ch < a.d) ra_store4(yr + ch, a.d - ch, v);
+            if (ch < a.d) ra_store4<R::DMA>(yr + ch, a.d - ch, v);
         }
     }
 }
@@ -507,12 +521,11 @@ struct RaDiagonals {
 // delta: dy . y has the rounding of a bfloat16 y in it.  dq and dk do not mind, but in the sums over buckets most of ds cancels, and that error does not.  So
 // the sum of a row's ds, which is 0 but for delta's error, corrects it: the sums of tiles beyond the reach afterwards, with those of p beside them,
 // while the tiles within the reach are gone through once more.  (Float: y is as exact as the rest, one walk does it all.)
-template <typename T, int DP, int WK>
+template <typename T, int DP, int WK, bool DMA>
 __global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_q(AttnArgs a) {
-    typedef Ra<T, DP, WK> R;
+    typedef Ra<T, DP, WK, DMA> R;
     extern __shared__ __attribute__((aligned(16))) unsigned char ra_lds[];
-    unsigned char *kt = ra_lds, *vt = ra_lds + R::TILE;
-    float* areas = reinterpret_cast<float*>(ra_lds + 2 * R::TILE);
+    float* areas = reinterpret_cast<float*>(ra_lds + R::LDS);
     float* lut = areas + RA_WAVES * 63 * RA_DIAG_PITCH;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 31, g = lane >> 5, wq = wave / WK, wk = wave % WK;
     float* area = areas + wave * 63 * RA_DIAG_PITCH;
@@ -530,9 +543,9 @@ __global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_q(AttnArgs a) {
     if (a.causal) end = ra_clamp(block_qmax + 1, 0, keys);
     const int all = (end + R::BN - 1) / R::BN;
     RaTile<T, R> kr, vr;
-    kr.place(a.ldk, a.d);
-    vr.place(a.ldv, a.d);
-    if (all > 0) { kr.load(kb, a.ldk, 0, end, a.d); vr.load(vb, a.ldv, 0, end, a.d); }
+    kr.place(ra_lds, a.ldk, a.d);
+    vr.place(ra_lds + R::TILE, a.ldv, a.d);
+    if (all > 0) { kr.load(kb, a.ldk, 0, end, a.d, 0); vr.load(vb, a.ldv, 0, end, a.d, 0); }
     const int64_t row = ((int64_t)n * a.H + h) * a.pq + i, first = ((int64_t)n * a.pq + i0) * a.ldy + (int64_t)h * a.d;
     RaRows<T, R> qr, gr;
     qr.load((const T*)a.q + ((int64_t)n * a.pq + i0) * a.ldq + (int64_t)h * a.d, a.ldq, l, mine, min(32, a.pq - i0), a.d, g);
@@ -563,7 +576,7 @@ __global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_q(AttnArgs a) {
     mm_f16 dq[R::DT] = {};
     float rowsum = 0.f, far_lo = 0.f, far_hi = 0.f;        // sums of ds over the row, of p beyond the reach on either side
     // p (dp - delta) of one 32 x 32 tile, and p's sum
-    auto scores = [&](int at, int j0, float (&ds)[16], float& psum) __attribute__((always_inline)) {
+    auto scores = [&](const unsigned char* kt, const unsigned char* vt, int at, int j0, float (&ds)[16], float& psum) __attribute__((always_inline)) {
         const mm_f16 s = ra_products<T, R>(kt, at, qr, lane), dp = ra_products<T, R>(vt, at, gr, lane);
         const bool far = ra_far(a.reach, j0 - qmax, j0 + 31 - qmin);
         const float one = lut[RA_PAD + (j0 - qmax >= a.reach ? 2 * a.reach : 0)];
@@ -597,17 +610,18 @@ __global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_q(AttnArgs a) {
         return far;
     };
     for (int t = 0; t < all; ++t) {
+        const unsigned char *kt = ra_lds + (t & 1) * 2 * R::TILE, *vt = kt + R::TILE;
+        kr.done(a.d, t & 1);
+        vr.done(a.d, t & 1);
+        ra_landed<R>();
         __syncthreads();
-        kr.store(kt, a.d);
-        vr.store(vt, a.d);
-        __syncthreads();
-        if (t + 1 < all) { kr.load(kb, a.ldk, (t + 1) * R::BN, end, a.d); vr.load(vb, a.ldv, (t + 1) * R::BN, end, a.d); }
+        if (t + 1 < all) { kr.load(kb, a.ldk, (t + 1) * R::BN, end, a.d, (t + 1) & 1); vr.load(vb, a.ldv, (t + 1) * R::BN, end, a.d, (t + 1) & 1); }
 #pragma unroll 1
         for (int u = 0; u < R::SUB; ++u) {
             const int at = (wk * R::SUB + u) * 32, j0 = t * R::BN + at;
             if (!work || j0 >= end || (a.causal && j0 > qmax)) continue;
             float ds[16], psum;
-            const bool far = scores(at, j0, ds, psum);
+            const bool far = scores(kt, vt, at, j0, ds, psum);
             if (dg.line) {
                 float s = 0.f;
 #pragma unroll
@@ -636,26 +650,28 @@ __global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_q(AttnArgs a) {
         dg.hi = fmaf(-rowsum, far_hi, dg.hi);
         // the tiles with distances within the reach of some query of the block
         const int t0 = ra_clamp(block_qmin - a.reach, 0, end) / R::BN, t1 = min(all, ra_clamp(block_qmax + a.reach, 0, end) / R::BN + 1);
-        if (t0 < t1) { kr.load(kb, a.ldk, t0 * R::BN, end, a.d); vr.load(vb, a.ldv, t0 * R::BN, end, a.d); }
+        __syncthreads();                   // (the tiles before have been read)
+        if (t0 < t1) { kr.load(kb, a.ldk, t0 * R::BN, end, a.d, t0 & 1); vr.load(vb, a.ldv, t0 * R::BN, end, a.d, t0 & 1); }
         for (int t = t0; t < t1; ++t) {
+            const unsigned char *kt = ra_lds + (t & 1) * 2 * R::TILE, *vt = kt + R::TILE;
+            kr.done(a.d, t & 1);
+            vr.done(a.d, t & 1);
+            ra_landed<R>();
             __syncthreads();
-            kr.store(kt, a.d);
-            vr.store(vt, a.d);
-            __syncthreads();
-            if (t + 1 < t1) { kr.load(kb, a.ldk, (t + 1) * R::BN, end, a.d); vr.load(vb, a.ldv, (t + 1) * R::BN, end, a.d); }
+            if (t + 1 < t1) { kr.load(kb, a.ldk, (t + 1) * R::BN, end, a.d, (t + 1) & 1); vr.load(vb, a.ldv, (t + 1) * R::BN, end, a.d, (t + 1) & 1); }
 #pragma unroll 1
             for (int u = 0; u < R::SUB; ++u) {
                 const int at = (wk * R::SUB + u) * 32, j0 = t * R::BN + at;
                 if (!work || j0 >= end || (a.causal && j0 > qmax) || ra_far(a.reach, j0 - qmax, j0 + 31 - qmin)) continue;
                 float ds[16], psum;
-                scores(at, j0, ds, psum);
+                scores(kt, vt, at, j0, ds, psum);
                 dg.add(ds, j0 - qmin - 31, area, lane);
             }
         }
     }
     if (mine && g == 0 && wk == 0) a.delta[row] = delta;
     if (dg.line) dg.finish(lane);
-    ra_gather<R, WK>(dq, reinterpret_cast<float*>(ra_lds), wq, wk, lane);
+    ra_gather<R>(dq, reinterpret_cast<float*>(ra_lds), wq, wk, lane);
     if (!mine) return;
     T* out = (T*)a.dq + ((int64_t)n * a.pq + i) * a.ldq + (int64_t)h * a.d;
 #pragma unroll
@@ -665,19 +681,18 @@ __global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_q(AttnArgs a) {
         for (int e = 0; e < 16; e += 4) {
             const int ch = ra_channel(c, e, g);
             const float v[4] = {dq[c][e] * a.scale, dq[c][e + 1] * a.scale, dq[c][e + 2] * a.scale, dq[c][e + 3] * a.scale};
-            if (ch < a.d) ra_store4(out + ch, a.d - ch, v);
+            if (ch < a.d) ra_store4<R::DMA>(out + ch, a.d - ch, v);
         }
     }
 }
 
 // dk and dv of a block's keys: the queries of every head that shares them, one head after the other
-template <typename T, int DP, int WK>
+template <typename T, int DP, int WK, bool DMA>
 __global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_kv(AttnArgs a) {
-    typedef Ra<T, DP, WK> R;
+    typedef Ra<T, DP, WK, DMA> R;
     extern __shared__ __attribute__((aligned(16))) unsigned char ra_lds[];
-    unsigned char *qt = ra_lds, *gt = ra_lds + R::TILE;
-    float* rowv = reinterpret_cast<float*>(ra_lds + 2 * R::TILE);          // [3][BN]: top, -log2 sum, delta
-    float* lut = rowv + 3 * R::BN;
+    float* rowvs = reinterpret_cast<float*>(ra_lds + R::LDS);         // two of [3][BN]: top, -log2 sum, delta
+    float* lut = rowvs + 6 * R::BN;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 31, g = lane >> 5, wq = wave / WK, wk = wave % WK;
     const int tiles = (a.pk + R::BM - 1) / R::BM;
     const RaBlock b = ra_block(a.G, tiles, 1);
@@ -692,8 +707,8 @@ __global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_kv(AttnArgs a) {
     const int first = a.causal ? ra_clamp(b.tile * R::BM - start, 0, a.pq) : 0;       // no query before it sees one of the block's keys
     const int t0 = first / R::BN, t1 = b.tile * R::BM < keys ? (a.pq + R::BN - 1) / R::BN : 0;
     RaTile<T, R> qs, gs;
-    qs.place(a.ldq, a.d);
-    gs.place(a.ldy, a.d);
+    qs.place(ra_lds, a.ldq, a.d);
+    gs.place(ra_lds + R::TILE, a.ldy, a.d);
     for (int hh = 0; hh < share; ++hh) {
         const int h = hk * share + hh;
         const T* qb = (const T*)a.q + (int64_t)n * a.pq * a.ldq + (int64_t)h * a.d;
@@ -702,24 +717,26 @@ __global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_kv(AttnArgs a) {
         float2_ st = {0.f, -INFINITY};
         float dl = 0.f;
         auto load = [&](int t) __attribute__((always_inline)) {
-            qs.load(qb, a.ldq, t * R::BN, a.pq, a.d);
-            gs.load(gb, a.ldy, t * R::BN, a.pq, a.d);
+            qs.load(qb, a.ldq, t * R::BN, a.pq, a.d, t & 1);
+            gs.load(gb, a.ldy, t * R::BN, a.pq, a.d, t & 1);
             const int i = min(t * R::BN + min((int)threadIdx.x, R::BN - 1), a.pq - 1);      // (rows beyond the last are masked)
             st = a.stats[row0 + i];
             dl = a.delta[row0 + i];
         };
+        __syncthreads();                                   // (the tiles and the bias of the head before have been read)
         if (t0 < t1) load(t0);
-        __syncthreads();                                   // (the bias of the head before has been read)
         ra_bias(a, h, 1, lut);
         for (int t = t0; t < t1; ++t) {
-            __syncthreads();
-            qs.store(qt, a.d);
-            gs.store(gt, a.d);
+            const unsigned char *qt = ra_lds + (t & 1) * 2 * R::TILE, *gt = qt + R::TILE;
+            float* rowv = rowvs + (t & 1) * 3 * R::BN;
+            qs.done(a.d, t & 1);
+            gs.done(a.d, t & 1);
             if ((int)threadIdx.x < R::BN) {
                 rowv[threadIdx.x] = st.y == -INFINITY ? 0.f : st.x;
                 rowv[R::BN + threadIdx.x] = st.y;
                 rowv[2 * R::BN + threadIdx.x] = dl;
             }
+            ra_landed<R>();
             __syncthreads();
             if (t + 1 < t1) load(t + 1);
 #pragma unroll 1
@@ -766,8 +783,8 @@ __global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_kv(AttnArgs a) {
             }
         }
     }
-    ra_gather<R, WK>(dk, reinterpret_cast<float*>(ra_lds), wq, wk, lane);
-    ra_gather<R, WK>(dv, reinterpret_cast<float*>(ra_lds), wq, wk, lane);
+    ra_gather<R>(dk, reinterpret_cast<float*>(ra_lds), wq, wk, lane);
+    ra_gather<R>(dv, reinterpret_cast<float*>(ra_lds), wq, wk, lane);
     if (j0 + l >= a.pk) return;                            // (keys behind the last one of the sample have gradients of zero)
     T* ok = (T*)a.dk + ((int64_t)n * a.pk + j) * a.ldk + (int64_t)hk * a.d;
     T* ov = (T*)a.dv + ((int64_t)n * a.pk + j) * a.ldv + (int64_t)hk * a.d;
@@ -779,7 +796,7 @@ __global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_kv(AttnArgs a) {
             const int ch = ra_channel(c, e, g);
             const float vk[4] = {dk[c][e] * a.scale, dk[c][e + 1] * a.scale, dk[c][e + 2] * a.scale, dk[c][e + 3] * a.scale};
             const float vv[4] = {dv[c][e], dv[c][e + 1], dv[c][e + 2], dv[c][e + 3]};
-            if (ch < a.d) { ra_store4(ok + ch, a.d - ch, vk); ra_store4(ov + ch, a.d - ch, vv); }
+            if (ch < a.d) { ra_store4<R::DMA>(ok + ch, a.d - ch, vk); ra_store4<R::DMA>(ov + ch, a.d - ch, vv); }
         }
     }
 }
@@ -822,11 +839,13 @@ __global__ void __launch_bounds__(RA_THREADS) relattn_buckets(const float* __res
 
 static size_t ra_up(size_t b) { return (b + 255) & ~(size_t)255; }
 // Wavefronts that share rows (and walk the other side's tiles together): where blocks of 128 rows are too few to give every CU two.
-template <typename T> constexpr int ra_wide() { return sizeof(T) == 2 ? 4 : 2; }
+// (As many as the tiles leave room for in LDS.)
+template <typename T, int DP> constexpr int ra_wide() { return sizeof(T) == 2 ? (DP <= 64 ? 4 : 2) : DP <= 64 ? 2 : 1; }
+static int ra_dp(int d, bool dma) { return d <= 32 && dma ? 32 : d <= 64 ? 64 : d <= 96 && dma ? 96 : 128; }
+static int ra_wide_of(int32_t dtype, int dp) { return dtype == LPM_BF16 ? (dp <= 64 ? 4 : 2) : dp <= 64 ? 2 : 1; }
 static bool ra_shared(int64_t blocks) { return blocks < 512; }
-static int ra_bm(int32_t dtype, int64_t pairs, int rows) {
-    return ra_shared(pairs * ((rows + 127) / 128)) ? 128 / (dtype == LPM_BF16 ? 4 : 2) : 128;
-}
+// (rows of a block do not depend on whether tiles go straight to LDS: scratch is sized without the operands)
+static int ra_bm(int32_t dtype, int d, int64_t pairs, int rows) { return ra_shared(pairs * ((rows + 127) / 128)) ? 128 / ra_wide_of(dtype, ra_dp(d, false)) : 128; }
 // The forward pass's blocks: rows folded over the heads that share keys where these fit two operands of 32 rows, and the keys over several blocks where they
 // are long and the blocks do not fill the card.
 struct RaForward { bool fold; int bm, splits; };
@@ -836,7 +855,7 @@ static RaForward ra_plan(const lpm_attn_geom& g, int32_t dtype) {
     f.fold = share > 1 && g.pq <= 32 && share * g.pq <= 64 && share * ra_lut(g.reach) <= 8192;
     const int rows = f.fold ? share * g.pq : g.pq;
     const int64_t pairs = (int64_t)g.m * (f.fold ? g.kv_heads : g.heads);
-    f.bm = ra_bm(dtype, pairs, rows);
+    f.bm = ra_bm(dtype, g.d, pairs, rows);
     const int64_t blocks = std::max<int64_t>(1, pairs * ((rows + f.bm - 1) / f.bm));
     f.splits = blocks >= 512 ? 1 : (int)std::min<int64_t>({std::max(1, g.pk / 512), (1024 + blocks - 1) / blocks, RA_MAX_SPLITS});
     return f;
@@ -846,7 +865,7 @@ static AttnLayout ra_layout(const lpm_attn_geom& g, int32_t dtype) {
     AttnLayout o;
     const RaForward f = ra_plan(g, dtype);
     const size_t rows = (size_t)g.m * g.heads * g.pq, nd = ra_distances(g.reach);
-    const int bm = ra_bm(dtype, (int64_t)g.m * g.heads, g.pq);
+    const int bm = ra_bm(dtype, g.d, (int64_t)g.m * g.heads, g.pq);
     o.lines = (g.pq + bm - 1) / bm * RA_WAVES;
     o.part_ml = f.splits > 1 ? ra_up((size_t)f.splits * rows * g.d * 4) : 0;
     o.fwd_all = f.splits > 1 ? o.part_ml + ra_up((size_t)f.splits * rows * 8) : 0;
@@ -863,32 +882,38 @@ template <typename K> static hipError_t ra_launch(K kernel, DeviceSet& done, int
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(RA_THREADS), lds, st, a);
     return hipGetLastError();
 }
-template <typename T, int DP, int WK> static hipError_t ra_forward(const AttnArgs& a, hipStream_t st) {
-    typedef Ra<T, DP, WK> R;
+template <typename T, int DP, int WK, bool DMA> static hipError_t ra_forward(const AttnArgs& a, hipStream_t st) {
+    typedef Ra<T, DP, WK, DMA> R;
     static DeviceSet done;
     const int share = a.H / a.G, rows = a.fold ? share * a.pq : a.pq;
-    return ra_launch(relattn_fwd<T, DP, WK>, done, (int64_t)a.m * (a.fold ? a.G : a.H) * ((rows + R::BM - 1) / R::BM) * a.splits,
-                     2 * R::TILE + (size_t)(a.fold ? share : 1) * ra_lut(a.reach) * 4, a, st);
+    return ra_launch(relattn_fwd<T, DP, WK, DMA>, done, (int64_t)a.m * (a.fold ? a.G : a.H) * ((rows + R::BM - 1) / R::BM) * a.splits,
+                     R::LDS + (size_t)(a.fold ? share : 1) * ra_lut(a.reach) * 4, a, st);
 }
-template <typename T, int DP, int WK> static hipError_t ra_backward_q(const AttnArgs& a, hipStream_t st) {
-    typedef Ra<T, DP, WK> R;
+template <typename T, int DP, int WK, bool DMA> static hipError_t ra_backward_q(const AttnArgs& a, hipStream_t st) {
+    typedef Ra<T, DP, WK, DMA> R;
     static DeviceSet done;
-    static_assert(2 * R::TILE + RA_WAVES * 63 * RA_DIAG_PITCH * 4 + (2 * RA_MAX_REACH + 1 + 2 * RA_PAD) * 4 <= 160 * 1024, "the tiles, diagonals and bias fit");
-    static_assert(WK == 1 || 128 / WK / 32 * WK * R::DT * 4096 <= 2 * R::TILE, "the sums of wavefronts that share rows fit over the tiles");
-    return ra_launch(relattn_bwd_q<T, DP, WK>, done, (int64_t)a.m * a.H * ((a.pq + R::BM - 1) / R::BM),
-                     2 * R::TILE + RA_WAVES * 63 * RA_DIAG_PITCH * 4 + (size_t)ra_lut(a.reach) * 4, a, st);
+    static_assert(R::LDS + RA_WAVES * 63 * RA_DIAG_PITCH * 4 + (2 * RA_MAX_REACH + 1 + 2 * RA_PAD) * 4 <= 160 * 1024, "the tiles, diagonals and bias fit");
+    static_assert(WK == 1 || 128 / WK / 32 * WK * R::DT * 4096 <= R::LDS, "the sums of wavefronts that share rows fit over the tiles");
+    return ra_launch(relattn_bwd_q<T, DP, WK, DMA>, done, (int64_t)a.m * a.H * ((a.pq + R::BM - 1) / R::BM),
+                     R::LDS + RA_WAVES * 63 * RA_DIAG_PITCH * 4 + (size_t)ra_lut(a.reach) * 4, a, st);
 }
-template <typename T, int DP, int WK> static hipError_t ra_backward_kv(const AttnArgs& a, hipStream_t st) {
-    typedef Ra<T, DP, WK> R;
+template <typename T, int DP, int WK, bool DMA> static hipError_t ra_backward_kv(const AttnArgs& a, hipStream_t st) {
+    typedef Ra<T, DP, WK, DMA> R;
     static DeviceSet done;
-    return ra_launch(relattn_bwd_kv<T, DP, WK>, done, (int64_t)a.m * a.G * ((a.pk + R::BM - 1) / R::BM), 2 * R::TILE + (3 * R::BN + (size_t)ra_lut(a.reach)) * 4, a, st);
+    return ra_launch(relattn_bwd_kv<T, DP, WK, DMA>, done, (int64_t)a.m * a.G * ((a.pk + R::BM - 1) / R::BM), R::LDS + (6 * R::BN + (size_t)ra_lut(a.reach)) * 4, a, st);
 }
-// f<T, padded channels, wavefronts that share rows>
-#define LPM_RA_WIDE(f_, T_, DP_, shared_) ((shared_) ? f_<T_, DP_, ra_wide<T_>()>(a, st) : f_<T_, DP_, 1>(a, st))
-#define LPM_RA_CHANNELS(f_, T_, shared_)                                                                                   \
-    (a.d <= 32 ? LPM_RA_WIDE(f_, T_, 32, shared_) : a.d <= 64 ? LPM_RA_WIDE(f_, T_, 64, shared_)                          \
-     : a.d <= 96 ? LPM_RA_WIDE(f_, T_, 96, shared_) : LPM_RA_WIDE(f_, T_, 128, shared_))
-#define LPM_RA(f_, dtype_, shared_) ((dtype_) == LPM_BF16 ? LPM_RA_CHANNELS(f_, bf16_t, shared_) : LPM_RA_CHANNELS(f_, float, shared_))
+// Tiles straight to LDS: channels in whole chunks, every row of both operands on a whole dword
+static bool ra_dma(int32_t dtype, int d, const void* p, int64_t ldp, const void* q, int64_t ldq) {
+    const int es = dtype == LPM_BF16 ? 2 : 4;
+    return d % (16 / es) == 0 && ((uintptr_t)p | (uintptr_t)q | (uintptr_t)(ldp * es) | (uintptr_t)(ldq * es)) % 4 == 0;
+}
+// f<T, padded channels, wavefronts that share rows, DMA>
+#define LPM_RA_WIDE(f_, T_, DP_, shared_, dma_) ((shared_) ? f_<T_, DP_, ra_wide<T_, DP_>(), dma_>(a, st) : f_<T_, DP_, 1, dma_>(a, st))
+#define LPM_RA_CHANNELS(f_, T_, shared_, dma_)                                                                                                     \
+    (!(dma_) ? (a.d <= 64 ? LPM_RA_WIDE(f_, T_, 64, shared_, false) : LPM_RA_WIDE(f_, T_, 128, shared_, false))                                     \
+     : a.d <= 32 ? LPM_RA_WIDE(f_, T_, 32, shared_, true) : a.d <= 64 ? LPM_RA_WIDE(f_, T_, 64, shared_, true)                                      \
+     : a.d <= 96 ? LPM_RA_WIDE(f_, T_, 96, shared_, true) : LPM_RA_WIDE(f_, T_, 128, shared_, true))
+#define LPM_RA(f_, dtype_, shared_, dma_) ((dtype_) == LPM_BF16 ? LPM_RA_CHANNELS(f_, bf16_t, shared_, dma_) : LPM_RA_CHANNELS(f_, float, shared_, dma_))
 
 }  // namespace lpm
 
@@ -898,7 +923,7 @@ static int32_t ra_check(const lpm_attn_geom* g, int32_t dtype, lpm_attn_geom& o)
     o = *g;
     if (o.m < 0 || o.pq < 0 || o.pk < 0 || o.pq > (1 << 28) || o.pk > (1 << 28) || o.heads <= 0 || o.heads > 65535 || o.kv_heads <= 0 || o.heads % o.kv_heads)
         return fail(LPM_ESHAPE, "attention of %d samples, %d queries, %d keys, %d heads on %d", o.m, o.pq, o.pk, o.heads, o.kv_heads);
-    if (o.d < 1 || o.d > 128) return fail(LPM_ESHAPE, "heads of %d channels (1 to 128)", o.d);
+    if (o.d < 8 || o.d > 128) return fail(LPM_ESHAPE, "heads of %d channels (8 to 128)", o.d);
     if (o.n_buckets < 0 || o.n_buckets > 65536 || o.reach < 0 || o.reach > RA_MAX_REACH)
         return fail(LPM_ESHAPE, "%d buckets (0 to 65536) of distances up to %d (0 to %d)", o.n_buckets, o.reach, RA_MAX_REACH);
     if (!(o.scale >= 0.f) || o.scale > 1e30f) return fail(LPM_EINVAL, "scale must be a number of 0 (for 1 / sqrt(d)) or more");
@@ -976,7 +1001,8 @@ extern "C" int32_t lpm_attn_forward(const lpm_attn_geom* geom, int32_t dtype, co
     a.part = (float*)ws;
     a.part_ml = (float*)((char*)ws + ra_layout(g, dtype).part_ml);
     hipStream_t st = (hipStream_t)stream;
-    LPM_HIP(LPM_RA(ra_forward, dtype, plan.bm < 128));
+    const bool dma = ra_dma(dtype, g.d, k, g.ldk, v, g.ldv);
+    LPM_HIP(LPM_RA(ra_forward, dtype, plan.bm < 128, dma));
     if (a.splits > 1) {
         const dim3 grid((unsigned)(((int64_t)g.m * g.heads * g.pq + RA_WAVES - 1) / RA_WAVES));
         if (dtype == LPM_BF16) hipLaunchKernelGGL(relattn_join<bf16_t>, grid, dim3(RA_THREADS), 0, st, a);
@@ -1006,8 +1032,9 @@ extern "C" int32_t lpm_attn_backward(const lpm_attn_geom* geom, int32_t dtype, c
     a.delta = (float*)ws;
     a.diag = dtable ? (float*)((char*)ws + o.diag) : nullptr;
     hipStream_t st = (hipStream_t)stream;
-    if (queries) LPM_HIP(LPM_RA(ra_backward_q, dtype, ra_bm(dtype, (int64_t)g.m * g.heads, g.pq) < 128));
-    if (keys) LPM_HIP(LPM_RA(ra_backward_kv, dtype, ra_bm(dtype, (int64_t)g.m * g.kv_heads, g.pk) < 128));
+    const bool dma_k = ra_dma(dtype, g.d, k, g.ldk, v, g.ldv), dma_q = ra_dma(dtype, g.d, q, g.ldq, dy, g.ldy);
+    if (queries) LPM_HIP(LPM_RA(ra_backward_q, dtype, ra_bm(dtype, g.d, (int64_t)g.m * g.heads, g.pq) < 128, dma_k));
+    if (keys) LPM_HIP(LPM_RA(ra_backward_kv, dtype, ra_bm(dtype, g.d, (int64_t)g.m * g.kv_heads, g.pk) < 128, dma_q));
     if (dtable) {
         const int nd = 2 * g.reach + 1;
         float* shares = (float*)((char*)ws + o.shares);

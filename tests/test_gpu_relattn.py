@@ -169,7 +169,7 @@ SHAPES = [
     A(2, 2, 1, 65, 64, 40, causal=1),                                  # the first queries see few keys, the last all
     A(2, 4, 2, 64, 130, 33, pad=5, lens=[130, 0]),                     # odd strides, a sample without keys
     A(1, 1, 1, 130, 66, 64, causal=1, starts=[-20]),                   # the first 20 queries see nothing
-    A(3, 2, 2, 40, 40, 1, lens=[1, 40, 39], nb=3, reach=0),            # heads of one channel, one bucket distance
+    A(3, 2, 2, 40, 40, 9, lens=[1, 40, 39], nb=3, reach=0),            # heads of nine channels, one bucket distance
     A(1, 2, 2, 50, 50, 64, nb=0, reach=0),                             # no bias
     A(1, 3, 1, 129, 200, 96, causal=1, starts=[71], reach=17),
     A(1, 2, 1, 70, 260, 128, reach=100, lens=[257]),
