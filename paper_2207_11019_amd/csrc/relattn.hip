@@ -47,12 +47,12 @@ struct AttnArgs {
 
 // WK wavefronts share a block's 128 / WK rows, each with its 32 rows of every tile of the other side.  DMA: tiles go straight from memory to LDS (channels in
 // whole 16-byte chunks, rows on whole dwords); else by way of registers, where a row's last chunk is put in order.
-template <typename T, int DP, int WK_, bool DMA_> struct Ra {
+template <typename T, int DP, int WK_, bool DMA_, bool SMALL = false> struct Ra {
     static constexpr int WK = WK_;
     static constexpr bool DMA = DMA_;
     static constexpr int EPC = Mm<T>::EPC, CHUNKS = DP / EPC, KS = DP / (2 * EPC), ES = (int)sizeof(T);
     static constexpr int BM = 128 / WK;
-    static constexpr int BN = WK > 1 ? 32 * WK : ES == 2 ? 64 : 32;      // rows of a staged tile
+    static constexpr int BN = WK > 1 ? 32 * WK : ES == 2 && !SMALL ? 64 : 32;      // rows of a staged tile
     static constexpr int SUB = BN / (32 * WK);                // 32-row pieces of it that a wavefront takes
     static constexpr int ROW = DP * ES;                       // bytes
     static constexpr int TILE = BN * ROW;
@@ -229,33 +229,46 @@ __device__ __forceinline__ bool ra_any(bool v) {
 // The bias of `heads` heads from h on by distance, lut[head][rel + reach + RA_PAD], in units of log2.  Finite values stay finite (a mask of the type's
 // lowest value leaves a row of such values with equal probabilities, as the formula does).
 __host__ __device__ inline int ra_lut(int reach) { return 2 * reach + 1 + 2 * RA_PAD; }
-__device__ __forceinline__ void ra_bias(const AttnArgs& a, int h, int heads, float* lut) {
-    const int n = ra_lut(a.reach);
-    for (int t = threadIdx.x; t < n; t += RA_THREADS) {
-        const int id = a.table ? ra_clamp(a.map[ra_clamp(t - RA_PAD, 0, 2 * a.reach)], 0, a.nb - 1) : 0;
-        for (int k = 0; k < heads; ++k) {
-            float b = 0.f;
-            if (a.table) {
-                b = a.table[(int64_t)(h + k) * a.nb + id];
-                const float big = 3.402823466e38f;
-                b = fabsf(b) <= big ? fminf(fmaxf(b * RA_LOG2E, -big), big) : b;
-            }
-            lut[k * n + t] = b;
+struct RaBias {
+    static constexpr int EARLY = 2;        // entries of a thread whose buckets are on their way from the kernel's beginning on
+    int id[EARLY];
+    __device__ __forceinline__ int bucket(const AttnArgs& a, int t) const { return ra_clamp(a.map[ra_clamp(t - RA_PAD, 0, 2 * a.reach)], 0, a.nb - 1); }
+    __device__ __forceinline__ void begin(const AttnArgs& a) {
+#pragma unroll
+        for (int k = 0; k < EARLY; ++k) id[k] = a.table ? a.map[ra_clamp((int)threadIdx.x + k * RA_THREADS - RA_PAD, 0, 2 * a.reach)] : 0;
+    }
+    static __device__ __forceinline__ float units(float b) {
+        const float big = 3.402823466e38f;
+        return fabsf(b) <= big ? fminf(fmaxf(b * RA_LOG2E, -big), big) : b;
+    }
+    __device__ __forceinline__ void store(const AttnArgs& a, int h, int heads, float* lut) const {
+        const int n = ra_lut(a.reach), first = (int)threadIdx.x;
+        for (int hh = 0; hh < heads; ++hh) {
+            const float* row = a.table ? a.table + (int64_t)(h + hh) * a.nb : nullptr;
+            float b[EARLY];
+#pragma unroll
+            for (int k = 0; k < EARLY; ++k) b[k] = row ? row[ra_clamp(id[k], 0, a.nb - 1)] : 0.f;
+#pragma unroll
+            for (int k = 0; k < EARLY; ++k) if (first + k * RA_THREADS < n) lut[hh * n + first + k * RA_THREADS] = units(b[k]);
+            for (int t = first + EARLY * RA_THREADS; t < n; t += RA_THREADS) lut[hh * n + t] = row ? units(row[bucket(a, t)]) : 0.f;
         }
     }
-}
+};
 // whether all distances relmin .. relmax have one bias
 __device__ __forceinline__ bool ra_far(int reach, int relmin, int relmax) { return relmax <= -reach || relmin >= reach; }
 
 __host__ __device__ inline int64_t ra_distances(int reach) { return 2 * (int64_t)reach + 1; }
 
+// Blocks of one head lie on one XCD one after the other, those with many visible keys (causal) and those with few in turn, so that every XCD has as much
+// to do whatever part of a head it gets.
 struct RaBlock { int n, h, tile, split; };
-__device__ __forceinline__ RaBlock ra_block(int heads, int tiles, int splits) {
+__device__ __forceinline__ RaBlock ra_block(int heads, int tiles, int splits, bool causal) {
     const int b = xcd_remap((int)blockIdx.x, (int)gridDim.x);
     RaBlock r;
     r.split = b % splits;
     const int x = b / splits, y = x / tiles;
-    r.tile = x - y * tiles;
+    const int t = x - y * tiles;
+    r.tile = !causal ? t : t & 1 ? t >> 1 : tiles - 1 - (t >> 1);
     r.h = y % heads;
     r.n = y / heads;
     return r;
@@ -267,9 +280,10 @@ __global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
     extern __shared__ __attribute__((aligned(16))) unsigned char ra_lds[];
     float* lut = reinterpret_cast<float*>(ra_lds + R::LDS);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 31, g = lane >> 5, wq = wave / WK, wk = wave % WK;
+    RaBias bias;
+    bias.begin(a);
     const int share = a.H / a.G, rows = a.fold ? share * a.pq : a.pq, tiles = (rows + R::BM - 1) / R::BM;
-    RaBlock b = ra_block(a.fold ? a.G : a.H, tiles, a.splits);
-    if (a.causal) b.tile = tiles - 1 - b.tile;             // (the blocks with the most keys first)
+    const RaBlock b = ra_block(a.fold ? a.G : a.H, tiles, a.splits, a.causal);
     const int n = b.n, hk = a.fold ? b.h : b.h / share, h0 = a.fold ? hk * share : b.h;
     const int r0 = b.tile * R::BM + wq * 32, r = min(r0 + l, rows - 1);
     const int hh = a.fold ? r / a.pq : 0, i = r - hh * a.pq, h = h0 + hh;
@@ -290,7 +304,7 @@ __global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
         qr.load((const T*)a.q + ((int64_t)n * a.pq + i) * a.ldq + (int64_t)h * a.d, 0, 0, work, 1, a.d, g);
     else
         qr.load((const T*)a.q + ((int64_t)n * a.pq + r0) * a.ldq + (int64_t)h * a.d, a.ldq, i - r0, work, min(32, a.pq - r0), a.d, g);
-    ra_bias(a, h0, a.fold ? share : 1, lut);
+    bias.store(a, h0, a.fold ? share : 1, lut);
     lut += hh * ra_lut(a.reach);
     mm_f16 o[R::DT] = {};
     float top = -INFINITY, sum = 0.f;
@@ -522,16 +536,17 @@ struct RaDiagonals {
 // the sum of a row's ds, which is 0 but for delta's error, corrects it: the sums of tiles beyond the reach afterwards, with those of p beside them,
 // while the tiles within the reach are gone through once more.  (Float: y is as exact as the rest, one walk does it all.)
 template <typename T, int DP, int WK, bool DMA>
-__global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_q(AttnArgs a) {
-    typedef Ra<T, DP, WK, DMA> R;
+__global__ void __launch_bounds__(RA_THREADS, sizeof(T) == 2 || DP <= 32 ? 2 : 1) relattn_bwd_q(AttnArgs a) {
+    typedef Ra<T, DP, WK, DMA, (DP > 64)> R;
     extern __shared__ __attribute__((aligned(16))) unsigned char ra_lds[];
     float* areas = reinterpret_cast<float*>(ra_lds + R::LDS);
     float* lut = areas + RA_WAVES * 63 * RA_DIAG_PITCH;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 31, g = lane >> 5, wq = wave / WK, wk = wave % WK;
+    RaBias bias;
+    bias.begin(a);
     float* area = areas + wave * 63 * RA_DIAG_PITCH;
     const int tiles = (a.pq + R::BM - 1) / R::BM;
-    RaBlock b = ra_block(a.H, tiles, 1);
-    if (a.causal) b.tile = tiles - 1 - b.tile;
+    const RaBlock b = ra_block(a.H, tiles, 1, a.causal);
     const int n = b.n, h = b.h, hk = h / (a.H / a.G);
     const int i0 = b.tile * R::BM + wq * 32, i = min(i0 + l, a.pq - 1);
     const bool work = i0 < a.pq, mine = i0 + l < a.pq;
@@ -568,8 +583,8 @@ __global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_q(AttnArgs a) {
     const bool some = stat.y != -INFINITY;                 // the query sees a key
     const float top = some ? stat.x : 0.f;
     const int least = !some ? -1 : a.causal ? min(keys - 1, qpos) : keys - 1;
-    ra_bias(a, h, 1, lut);
-    for (int t = lane; t < 63 * RA_DIAG_PITCH; t += 64) area[t] = 0.f;
+    bias.store(a, h, 1, lut);
+    for (int t = lane * 4; t < 63 * RA_DIAG_PITCH; t += 256) *reinterpret_cast<float4*>(area + t) = make_float4(0.f, 0.f, 0.f, 0.f);
     RaDiagonals dg;
     dg.reach = a.reach;
     dg.line = a.diag ? a.diag + (((int64_t)n * a.H + h) * tiles * RA_WAVES + b.tile * RA_WAVES + wave) * ra_distances(a.reach) : nullptr;
@@ -688,14 +703,16 @@ __global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_q(AttnArgs a) {
 
 // dk and dv of a block's keys: the queries of every head that shares them, one head after the other
 template <typename T, int DP, int WK, bool DMA>
-__global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_kv(AttnArgs a) {
+__global__ void __launch_bounds__(RA_THREADS, DP <= 32 || (sizeof(T) == 2 && DP <= 64) ? 2 : 1) relattn_bwd_kv(AttnArgs a) {
     typedef Ra<T, DP, WK, DMA> R;
     extern __shared__ __attribute__((aligned(16))) unsigned char ra_lds[];
     float* rowvs = reinterpret_cast<float*>(ra_lds + R::LDS);         // two of [3][BN]: top, -log2 sum, delta
     float* lut = rowvs + 6 * R::BN;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 31, g = lane >> 5, wq = wave / WK, wk = wave % WK;
+    RaBias bias;
+    bias.begin(a);
     const int tiles = (a.pk + R::BM - 1) / R::BM;
-    const RaBlock b = ra_block(a.G, tiles, 1);
+    const RaBlock b = ra_block(a.G, tiles, 1, a.causal);
     const int n = b.n, hk = b.h, share = a.H / a.G;
     const int j0 = b.tile * R::BM + wq * 32, j = min(j0 + l, a.pk - 1);
     const int start = ra_start(a, n), keys = ra_keys(a, n);
@@ -725,7 +742,7 @@ __global__ void __launch_bounds__(RA_THREADS, 1) relattn_bwd_kv(AttnArgs a) {
         };
         __syncthreads();                                   // (the tiles and the bias of the head before have been read)
         if (t0 < t1) load(t0);
-        ra_bias(a, h, 1, lut);
+        bias.store(a, h, 1, lut);
         for (int t = t0; t < t1; ++t) {
             const unsigned char *qt = ra_lds + (t & 1) * 2 * R::TILE, *gt = qt + R::TILE;
             float* rowv = rowvs + (t & 1) * 3 * R::BN;
@@ -821,16 +838,21 @@ __global__ void __launch_bounds__(RA_THREADS) relattn_diagonals(const float* __r
 __global__ void __launch_bounds__(RA_THREADS) relattn_buckets(const float* __restrict__ shares, const int32_t* __restrict__ map, int H, int nb, int nd,
                                                               float* __restrict__ dtable, int accumulate) {
     extern __shared__ __attribute__((aligned(16))) float ra_sums[];
+    int* ids = reinterpret_cast<int*>(ra_sums + nd);
     const int h = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int c = threadIdx.x; c < nd; c += RA_THREADS) {
-        float s = 0.f;
-        for (int k = 0; k < RA_SHARES; ++k) s += shares[((int64_t)k * H + h) * nd + c];
+        float v[RA_SHARES], s = 0.f;
+        ids[c] = ra_clamp(map[c], 0, nb - 1);
+#pragma unroll
+        for (int k = 0; k < RA_SHARES; ++k) v[k] = shares[((int64_t)k * H + h) * nd + c];
+#pragma unroll
+        for (int k = 0; k < RA_SHARES; ++k) s += v[k];
         ra_sums[c] = s;
     }
     __syncthreads();
     for (int b = wave; b < nb; b += RA_WAVES) {
         float s = 0.f;
-        for (int c = lane; c < nd; c += 64) if (ra_clamp(map[c], 0, nb - 1) == b) s += ra_sums[c];
+        for (int c = lane; c < nd; c += 64) s += ids[c] == b ? ra_sums[c] : 0.f;
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
         if (lane == 0) dtable[(int64_t)h * nb + b] = accumulate ? dtable[(int64_t)h * nb + b] + s : s;
@@ -843,7 +865,7 @@ static size_t ra_up(size_t b) { return (b + 255) & ~(size_t)255; }
 template <typename T, int DP> constexpr int ra_wide() { return sizeof(T) == 2 ? (DP <= 64 ? 4 : 2) : DP <= 64 ? 2 : 1; }
 static int ra_dp(int d, bool dma) { return d <= 32 && dma ? 32 : d <= 64 ? 64 : d <= 96 && dma ? 96 : 128; }
 static int ra_wide_of(int32_t dtype, int dp) { return dtype == LPM_BF16 ? (dp <= 64 ? 4 : 2) : dp <= 64 ? 2 : 1; }
-static bool ra_shared(int64_t blocks) { return blocks < 512; }
+static bool ra_shared(int64_t blocks) { return blocks < 256; }
 // (rows of a block do not depend on whether tiles go straight to LDS: scratch is sized without the operands)
 static int ra_bm(int32_t dtype, int d, int64_t pairs, int rows) { return ra_shared(pairs * ((rows + 127) / 128)) ? 128 / ra_wide_of(dtype, ra_dp(d, false)) : 128; }
 // The forward pass's blocks: rows folded over the heads that share keys where these fit two operands of 32 rows, and the keys over several blocks where they
@@ -890,7 +912,7 @@ template <typename T, int DP, int WK, bool DMA> static hipError_t ra_forward(con
                      R::LDS + (size_t)(a.fold ? share : 1) * ra_lut(a.reach) * 4, a, st);
 }
 template <typename T, int DP, int WK, bool DMA> static hipError_t ra_backward_q(const AttnArgs& a, hipStream_t st) {
-    typedef Ra<T, DP, WK, DMA> R;
+    typedef Ra<T, DP, WK, DMA, (DP > 64)> R;
     static DeviceSet done;
     static_assert(R::LDS + RA_WAVES * 63 * RA_DIAG_PITCH * 4 + (2 * RA_MAX_REACH + 1 + 2 * RA_PAD) * 4 <= 160 * 1024, "the tiles, diagonals and bias fit");
     static_assert(WK == 1 || 128 / WK / 32 * WK * R::DT * 4096 <= R::LDS, "the sums of wavefronts that share rows fit over the tiles");
@@ -1040,7 +1062,7 @@ extern "C" int32_t lpm_attn_backward(const lpm_attn_geom* geom, int32_t dtype, c
         float* shares = (float*)((char*)ws + o.shares);
         hipLaunchKernelGGL(relattn_diagonals, dim3((unsigned)((nd + 63) / 64), (unsigned)g.heads, RA_SHARES), dim3(RA_THREADS), 0, st, (const float*)a.diag, g.m,
                            g.heads, o.lines, nd, shares);
-        hipLaunchKernelGGL(relattn_buckets, dim3((unsigned)g.heads), dim3(RA_THREADS), (size_t)nd * 4, st, (const float*)shares, map, g.heads, g.n_buckets, nd, dtable,
+        hipLaunchKernelGGL(relattn_buckets, dim3((unsigned)g.heads), dim3(RA_THREADS), (size_t)nd * 8, st, (const float*)shares, map, g.heads, g.n_buckets, nd, dtable,
                            accumulate);
         LPM_HIP(hipGetLastError());
     }
