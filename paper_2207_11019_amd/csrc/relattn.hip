@@ -259,18 +259,40 @@ __device__ __forceinline__ bool ra_far(int reach, int relmin, int relmax) { retu
 
 __host__ __device__ inline int64_t ra_distances(int reach) { return 2 * (int64_t)reach + 1; }
 
-// Blocks of one head lie on one XCD one after the other, those with many visible keys (causal) and those with few in turn, so that every XCD has as much
-// to do whatever part of a head it gets.
+// Blocks of one head lie on one XCD, one after the other.  Causal: those with the most visible keys first, heads in turn (REVERSE: the last tiles have the
+// most), over as many heads as an XCD has -- all of them, where they do not come in eights.
+// A tile of scores is FAR: one bias for all of it and every pair visible; NEAR: a bias by distance, every pair visible; EDGE: any.
+enum { RA_FAR = 0, RA_NEAR = 1, RA_EDGE = 2 };
+template <int V> struct RaMode { static constexpr int value = V; };
+// f(mode) without a branch inside it, so that the reads of one product run beside the arithmetic of another
+template <typename F> __device__ __forceinline__ void ra_dispatch(bool edge, bool far, F&& f) {
+    if (edge) f(RaMode<RA_EDGE>());
+    else if (far) f(RaMode<RA_FAR>());
+    else f(RaMode<RA_NEAR>());
+}
+
 struct RaBlock { int n, h, tile, split; };
-__device__ __forceinline__ RaBlock ra_block(int heads, int tiles, int splits, bool causal) {
-    const int b = xcd_remap((int)blockIdx.x, (int)gridDim.x);
+template <bool REVERSE> __device__ __forceinline__ RaBlock ra_block(int m, int heads, int tiles, int splits, bool causal) {
+    const int pairs = m * heads;
     RaBlock r;
-    r.split = b % splits;
-    const int x = b / splits, y = x / tiles;
-    const int t = x - y * tiles;
-    r.tile = !causal ? t : t & 1 ? t >> 1 : tiles - 1 - (t >> 1);
-    r.h = y % heads;
-    r.n = y / heads;
+    int b = (int)blockIdx.x, pair;
+    if (!causal) {
+        b = xcd_remap(b, (int)gridDim.x);
+        r.split = b % splits;
+        b /= splits;
+        pair = b / tiles;
+        r.tile = b - pair * tiles;
+    } else {
+        r.split = b % splits;
+        b /= splits;
+        const int sets = pairs % 8 ? 1 : 8, per = pairs / sets, x = b % sets;
+        b /= sets;
+        const int t = b / per;
+        pair = x * per + (b - t * per);
+        r.tile = REVERSE ? tiles - 1 - t : t;
+    }
+    r.h = pair % heads;
+    r.n = pair / heads;
     return r;
 }
 
@@ -283,7 +305,7 @@ __global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
     RaBias bias;
     bias.begin(a);
     const int share = a.H / a.G, rows = a.fold ? share * a.pq : a.pq, tiles = (rows + R::BM - 1) / R::BM;
-    const RaBlock b = ra_block(a.fold ? a.G : a.H, tiles, a.splits, a.causal);
+    const RaBlock b = ra_block<true>(a.m, a.fold ? a.G : a.H, tiles, a.splits, a.causal);
     const int n = b.n, hk = a.fold ? b.h : b.h / share, h0 = a.fold ? hk * share : b.h;
     const int r0 = b.tile * R::BM + wq * 32, r = min(r0 + l, rows - 1);
     const int hh = a.fold ? r / a.pq : 0, i = r - hh * a.pq, h = h0 + hh;
@@ -318,62 +340,63 @@ __global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
         const int j0 = t * R::BN + wk * 32 * R::SUB;       // the wavefront's keys of the tile
         if (!work || j0 >= end || (a.causal && j0 > qmax)) continue;
         const int last = j0 + 32 * R::SUB - 1;
-        const bool edge = last >= keys || (a.causal && last > qmin);
-        float s[R::SUB][16];
-        float mx = -INFINITY;
         const bool far = ra_far(a.reach, j0 - qmax, last - qmin);
         const float one = lut[RA_PAD + (j0 - qmax >= a.reach ? 2 * a.reach : 0)];
-        const float* near = lut + (far ? 0 : j0 + 4 * g - qpos + a.reach + RA_PAD);
+        // (a bias of the order of the largest numbers swallows the score: only the way that adds the two first gives what the formula gives)
+        const bool edge = last >= keys || (a.causal && last > qmin) || (far && !(fabsf(one) < 1e30f));
+        ra_dispatch(edge, far, [&](auto mode) __attribute__((always_inline)) {
+            constexpr int MODE = decltype(mode)::value;
+            float s[R::SUB][16];
+            float mx = -INFINITY;
 #pragma unroll
-        for (int u = 0; u < R::SUB; ++u) {
-            const mm_f16 acc = ra_products<T, R>(kt, wk * 32 * R::SUB + 32 * u, qr, lane);
+            for (int u = 0; u < R::SUB; ++u) {
+                const mm_f16 acc = ra_products<T, R>(kt, wk * 32 * R::SUB + 32 * u, qr, lane);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[u][e] = acc[e];
-        }
-        if (far) {
+                for (int e = 0; e < 16; ++e) s[u][e] = acc[e];
+            }
+            if constexpr (MODE != RA_FAR) {
+                const float* near = lut + (far ? (j0 - qmax >= a.reach ? a.reach : -a.reach) : j0 + 4 * g - qpos) + a.reach + RA_PAD;
+                const int least = a.causal ? min(keys - 1, qpos) : keys - 1;      // the last key that this query sees
+#pragma unroll
+                for (int u = 0; u < R::SUB; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int at = 32 * u + (e & 3) + 8 * (e >> 2);
+                        s[u][e] = fmaf(s[u][e], a.scale2, MODE == RA_EDGE && far ? one : near[at]);
+                        if (MODE == RA_EDGE && j0 + 4 * g + at > least) s[u][e] = -INFINITY;
+                    }
+            }
 #pragma unroll
             for (int u = 0; u < R::SUB; ++u)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[u][e] = fmaf(s[u][e], a.scale2, one);
-        } else {
+                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[u][e]);
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            if (MODE == RA_FAR) mx = fmaf(mx, a.scale2, one);
+            // the reference moves only where a row's maximum has passed it by 2^8 (or it had none): until then p is up to 2^8, which float and
+            // bfloat16 hold as exactly as 1
+            if (ra_any(mx > top + 8.f || (top == -INFINITY && mx > top))) {
+                const float to = fmaxf(mx, top), base = to == -INFINITY ? 0.f : to, shrink = exp2_fast(top - base);
+                top = to;
+                sum *= shrink;
+#pragma unroll
+                for (int c = 0; c < R::DT; ++c)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[c][e] *= shrink;
+            }
+            const float base = top == -INFINITY ? 0.f : top, rest = one - base;
+            float part = 0.f;
 #pragma unroll
             for (int u = 0; u < R::SUB; ++u)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[u][e] = fmaf(s[u][e], a.scale2, near[32 * u + (e & 3) + 8 * (e >> 2)]);
-        }
-        if (edge) {
-            const int least = a.causal ? min(keys - 1, qpos) : keys - 1;      // the last key that this query sees
+                for (int e = 0; e < 16; ++e) {
+                    s[u][e] = exp2_fast(MODE == RA_FAR ? fmaf(s[u][e], a.scale2, rest) : s[u][e] - base);
+                    part += s[u][e];
+                }
+            sum += part;
+            // (p enters the product in the element type: for bfloat16 an error of 2^-9 of each term, below the rounding of y)
 #pragma unroll
-            for (int u = 0; u < R::SUB; ++u)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) if (j0 + 32 * u + 4 * g + (e & 3) + 8 * (e >> 2) > least) s[u][e] = -INFINITY;
-        }
-#pragma unroll
-        for (int u = 0; u < R::SUB; ++u)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[u][e]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        // the reference moves only where a row's maximum has passed it by 2^8 (or it had none): until then p is up to 2^8, which float and
-        // bfloat16 hold as exactly as 1
-        if (ra_any(mx > top + 8.f || (top == -INFINITY && mx > top))) {
-            const float to = fmaxf(mx, top), base = to == -INFINITY ? 0.f : to, shrink = exp2_fast(top - base);
-            top = to;
-            sum *= shrink;
-#pragma unroll
-            for (int c = 0; c < R::DT; ++c)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[c][e] *= shrink;
-        }
-        const float base = top == -INFINITY ? 0.f : top;
-        float part = 0.f;
-#pragma unroll
-        for (int u = 0; u < R::SUB; ++u)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) { s[u][e] = exp2_fast(s[u][e] - base); part += s[u][e]; }
-        sum += part;
-        // (p enters the product in the element type: for bfloat16 an error of 2^-9 of each term, below the rounding of y)
-#pragma unroll
-        for (int u = 0; u < R::SUB; ++u) ra_mix<T, R>(vt, wk * 32 * R::SUB + 32 * u, s[u], o, lane);
+            for (int u = 0; u < R::SUB; ++u) ra_mix<T, R>(vt, wk * 32 * R::SUB + 32 * u, s[u], o, lane);
+        });
     }
     sum += __shfl_xor(sum, 32, 64);
     if (WK > 1) {                           // one reference for the wavefronts that share the rows
@@ -546,7 +569,7 @@ __global__ void __launch_bounds__(RA_THREADS, sizeof(T) == 2 || DP <= 32 ? 2 : 1
     bias.begin(a);
     float* area = areas + wave * 63 * RA_DIAG_PITCH;
     const int tiles = (a.pq + R::BM - 1) / R::BM;
-    const RaBlock b = ra_block(a.H, tiles, 1, a.causal);
+    const RaBlock b = ra_block<true>(a.m, a.H, tiles, 1, a.causal);
     const int n = b.n, h = b.h, hk = h / (a.H / a.G);
     const int i0 = b.tile * R::BM + wq * 32, i = min(i0 + l, a.pq - 1);
     const bool work = i0 < a.pq, mine = i0 + l < a.pq;
@@ -590,40 +613,28 @@ __global__ void __launch_bounds__(RA_THREADS, sizeof(T) == 2 || DP <= 32 ? 2 : 1
     dg.line = a.diag ? a.diag + (((int64_t)n * a.H + h) * tiles * RA_WAVES + b.tile * RA_WAVES + wave) * ra_distances(a.reach) : nullptr;
     mm_f16 dq[R::DT] = {};
     float rowsum = 0.f, far_lo = 0.f, far_hi = 0.f;        // sums of ds over the row, of p beyond the reach on either side
-    // p (dp - delta) of one 32 x 32 tile, and p's sum
-    auto scores = [&](const unsigned char* kt, const unsigned char* vt, int at, int j0, float (&ds)[16], float& psum) __attribute__((always_inline)) {
+    // p (dp - delta) of one 32 x 32 tile, and p's sum (of a far one)
+    auto scores = [&](auto mode, const unsigned char* kt, const unsigned char* vt, int at, int j0, bool far, float (&ds)[16], float& psum) __attribute__((always_inline)) {
+        constexpr int MODE = decltype(mode)::value;
         const mm_f16 s = ra_products<T, R>(kt, at, qr, lane), dp = ra_products<T, R>(vt, at, gr, lane);
-        const bool far = ra_far(a.reach, j0 - qmax, j0 + 31 - qmin);
         const float one = lut[RA_PAD + (j0 - qmax >= a.reach ? 2 * a.reach : 0)];
         const float* near = lut + (far ? 0 : j0 + 4 * g - qpos + a.reach + RA_PAD);
-        float p[16];
-        if (far) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) p[e] = fmaf(s[e], a.scale2, one);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) p[e] = fmaf(s[e], a.scale2, near[(e & 3) + 8 * (e >> 2)]);
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) p[e] = exp2_fast((p[e] - top) + stat.y);
-        if (j0 + 31 >= keys || i0 + 32 > a.pq || (a.causal && j0 + 31 > qmin) || ra_any(!some)) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const bool seen = j0 + 4 * g + (e & 3) + 8 * (e >> 2) <= least;
-                p[e] = seen ? p[e] : 0.f;
-                ds[e] = seen ? p[e] * (dp[e] - delta) : 0.f;
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) ds[e] = p[e] * (dp[e] - delta);
-        }
         psum = 0.f;
-        if (far) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) psum += p[e];
+        for (int e = 0; e < 16; ++e) {
+            const int to = (e & 3) + 8 * (e >> 2);
+            float p = fmaf(s[e], a.scale2, MODE == RA_FAR || (MODE == RA_EDGE && far) ? one : near[to]);
+            p = exp2_fast((p - top) + stat.y);
+            ds[e] = p * (dp[e] - delta);
+            if (MODE == RA_EDGE) {
+                const bool seen = j0 + 4 * g + to <= least;
+                p = seen ? p : 0.f;
+                ds[e] = seen ? ds[e] : 0.f;
+            }
+            if (MODE != RA_NEAR) psum += p;
         }
-        return far;
     };
+    auto edge = [&](int j0) __attribute__((always_inline)) { return j0 + 31 >= keys || i0 + 32 > a.pq || (a.causal && j0 + 31 > qmin); };
     for (int t = 0; t < all; ++t) {
         const unsigned char *kt = ra_lds + (t & 1) * 2 * R::TILE, *vt = kt + R::TILE;
         kr.done(a.d, t & 1);
@@ -635,18 +646,22 @@ __global__ void __launch_bounds__(RA_THREADS, sizeof(T) == 2 || DP <= 32 ? 2 : 1
         for (int u = 0; u < R::SUB; ++u) {
             const int at = (wk * R::SUB + u) * 32, j0 = t * R::BN + at;
             if (!work || j0 >= end || (a.causal && j0 > qmax)) continue;
-            float ds[16], psum;
-            const bool far = scores(kt, vt, at, j0, ds, psum);
-            if (dg.line) {
-                float s = 0.f;
+            const bool far = ra_far(a.reach, j0 - qmax, j0 + 31 - qmin), behind = j0 - qmax >= a.reach;
+            ra_dispatch(edge(j0), far, [&](auto mode) __attribute__((always_inline)) {
+                float ds[16], psum, s = 0.f;
+                scores(mode, kt, vt, at, j0, far, ds, psum);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s += ds[e];
                 rowsum += s;
-                if (far && j0 - qmax >= a.reach) { dg.hi += s; far_hi += psum; }
-                else if (far) { dg.lo += s; far_lo += psum; }
-                else if (R::ES == 4) dg.add(ds, j0 - qmin - 31, area, lane);
-            }
-            ra_mix<T, R>(kt, at, ds, dq, lane);
+                if (decltype(mode)::value != RA_NEAR) {
+                    dg.hi += far && behind ? s : 0.f;
+                    far_hi += far && behind ? psum : 0.f;
+                    dg.lo += far && !behind ? s : 0.f;
+                    far_lo += far && !behind ? psum : 0.f;
+                }
+                if (R::ES == 4 && dg.line && !far) dg.add(ds, j0 - qmin - 31, area, lane);
+                ra_mix<T, R>(kt, at, ds, dq, lane);
+            });
         }
     }
     if (R::ES == 2 && dg.line) {
@@ -679,7 +694,8 @@ __global__ void __launch_bounds__(RA_THREADS, sizeof(T) == 2 || DP <= 32 ? 2 : 1
                 const int at = (wk * R::SUB + u) * 32, j0 = t * R::BN + at;
                 if (!work || j0 >= end || (a.causal && j0 > qmax) || ra_far(a.reach, j0 - qmax, j0 + 31 - qmin)) continue;
                 float ds[16], psum;
-                scores(kt, vt, at, j0, ds, psum);
+                if (edge(j0)) scores(RaMode<RA_EDGE>(), kt, vt, at, j0, false, ds, psum);
+                else scores(RaMode<RA_NEAR>(), kt, vt, at, j0, false, ds, psum);
                 dg.add(ds, j0 - qmin - 31, area, lane);
             }
         }
@@ -712,7 +728,7 @@ __global__ void __launch_bounds__(RA_THREADS, DP <= 32 || (sizeof(T) == 2 && DP 
     RaBias bias;
     bias.begin(a);
     const int tiles = (a.pk + R::BM - 1) / R::BM;
-    const RaBlock b = ra_block(a.G, tiles, 1, a.causal);
+    const RaBlock b = ra_block<false>(a.m, a.G, tiles, 1, a.causal);
     const int n = b.n, hk = b.h, share = a.H / a.G;
     const int j0 = b.tile * R::BM + wq * 32, j = min(j0 + l, a.pk - 1);
     const int start = ra_start(a, n), keys = ra_keys(a, n);
@@ -760,43 +776,36 @@ __global__ void __launch_bounds__(RA_THREADS, DP <= 32 || (sizeof(T) == 2 && DP 
             for (int u = 0; u < R::SUB; ++u) {
                 const int at = (wk * R::SUB + u) * 32, i0 = t * R::BN + at, qmin = i0 + start, qmax = min(i0 + 31, a.pq - 1) + start;
                 if (!work || i0 >= a.pq || (a.causal && j0 > qmax)) continue;
-                const mm_f16 s = ra_products<T, R>(qt, at, kr, lane), dp = ra_products<T, R>(gt, at, vr, lane);
                 const bool far = ra_far(a.reach, j0 - i0 - start - 31, j0 + 31 - qmin);
-                const float one = lut[RA_PAD + (j0 - i0 - start - 31 >= a.reach ? 2 * a.reach : 0)];
-                const float* near = lut + (far ? 64 : j0 + l - i0 - start - 4 * g + a.reach + RA_PAD);
-                float p[16], ds[16];
-                if (far) {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) p[e] = fmaf(s[e], a.scale2, one);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) p[e] = fmaf(s[e], a.scale2, near[-((e & 3) + 8 * (e >> 2))]);
-                }
-                bool empty = false;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const float* rv = rowv + at + 8 * c + 4 * g;
-                    const float4 tp = *reinterpret_cast<const float4*>(rv), ls = *reinterpret_cast<const float4*>(rv + R::BN), de = *reinterpret_cast<const float4*>(rv + 2 * R::BN);
-                    const float tops[4] = {tp.x, tp.y, tp.z, tp.w}, logs[4] = {ls.x, ls.y, ls.z, ls.w}, deltas[4] = {de.x, de.y, de.z, de.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        p[4 * c + e] = exp2_fast((p[4 * c + e] - tops[e]) + logs[e]);
-                        ds[4 * c + e] = p[4 * c + e] * (dp[4 * c + e] - deltas[e]);
-                        empty |= logs[e] == -INFINITY;
-                    }
-                }
-                if (j0 + 32 > keys || i0 + 32 > a.pq || (a.causal && j0 + 31 > qmin) || ra_any(empty)) {
+                const bool edge = j0 + 32 > keys || i0 + 32 > a.pq || (a.causal && j0 + 31 > qmin);
+                ra_dispatch(edge, far, [&](auto mode) __attribute__((always_inline)) {
+                    constexpr int MODE = decltype(mode)::value;
+                    const mm_f16 s = ra_products<T, R>(qt, at, kr, lane), dp = ra_products<T, R>(gt, at, vr, lane);
+                    const float one = lut[RA_PAD + (j0 - i0 - start - 31 >= a.reach ? 2 * a.reach : 0)];
+                    const float* near = lut + (far ? 64 : j0 + l - i0 - start - 4 * g + a.reach + RA_PAD);
                     const int from = a.causal ? j0 + l - start : 0;      // the first query that sees this key
+                    float p[16], ds[16];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int ii = 4 * g + (e & 3) + 8 * (e >> 2);
-                        const bool seen = mine && i0 + ii < a.pq && i0 + ii >= from && rowv[R::BN + at + ii] != -INFINITY;
-                        p[e] = seen ? p[e] : 0.f;
-                        ds[e] = seen ? ds[e] : 0.f;
+                    for (int c = 0; c < 4; ++c) {
+                        const float* rv = rowv + at + 8 * c + 4 * g;
+                        const float4 tp = *reinterpret_cast<const float4*>(rv), ls = *reinterpret_cast<const float4*>(rv + R::BN), de = *reinterpret_cast<const float4*>(rv + 2 * R::BN);
+                        const float tops[4] = {tp.x, tp.y, tp.z, tp.w}, logs[4] = {ls.x, ls.y, ls.z, ls.w}, deltas[4] = {de.x, de.y, de.z, de.w};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int e = 4 * c + k, i = i0 + 4 * g + k + 8 * c;
+                            const float v = fmaf(s[e], a.scale2, MODE == RA_FAR || (MODE == RA_EDGE && far) ? one : near[-(k + 8 * c)]);
+                            p[e] = exp2_fast((v - tops[k]) + logs[k]);
+                            ds[e] = p[e] * (dp[e] - deltas[k]);
+                            if (MODE == RA_EDGE) {
+                                const bool seen = mine && i < a.pq && i >= from && logs[k] != -INFINITY;
+                                p[e] = seen ? p[e] : 0.f;
+                                ds[e] = seen ? ds[e] : 0.f;
+                            }
+                        }
                     }
-                }
-                ra_mix<T, R>(gt, at, p, dv, lane);
-                ra_mix<T, R>(qt, at, ds, dk, lane);
+                    ra_mix<T, R>(gt, at, p, dv, lane);
+                    ra_mix<T, R>(qt, at, ds, dk, lane);
+                });
             }
         }
     }
@@ -865,7 +874,7 @@ static size_t ra_up(size_t b) { return (b + 255) & ~(size_t)255; }
 template <typename T, int DP> constexpr int ra_wide() { return sizeof(T) == 2 ? (DP <= 64 ? 4 : 2) : DP <= 64 ? 2 : 1; }
 static int ra_dp(int d, bool dma) { return d <= 32 && dma ? 32 : d <= 64 ? 64 : d <= 96 && dma ? 96 : 128; }
 static int ra_wide_of(int32_t dtype, int dp) { return dtype == LPM_BF16 ? (dp <= 64 ? 4 : 2) : dp <= 64 ? 2 : 1; }
-static bool ra_shared(int64_t blocks) { return blocks < 256; }
+static bool ra_shared(int64_t blocks) { return blocks <= 256; }
 // (rows of a block do not depend on whether tiles go straight to LDS: scratch is sized without the operands)
 static int ra_bm(int32_t dtype, int d, int64_t pairs, int rows) { return ra_shared(pairs * ((rows + 127) / 128)) ? 128 / ra_wide_of(dtype, ra_dp(d, false)) : 128; }
 // The forward pass's blocks: rows folded over the heads that share keys where these fit two operands of 32 rows, and the keys over several blocks where they
