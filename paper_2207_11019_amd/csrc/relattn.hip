@@ -60,8 +60,11 @@ template <typename T, int DP, int WK_, bool DMA_, bool SMALL = false> struct Ra 
     static constexpr int LDS = 2 * STAGES * TILE;             // tiles of both operands
     static constexpr int PER = BN * CHUNKS / RA_THREADS;      // chunks of a tile a thread brings
     static constexpr int DT = DP / 32;                        // 32-channel pieces of a head
-    // Chunk c of a row lies at position c ^ place(row): eight consecutive rows at one chunk, and four at two neighbouring ones, are on distinct banks.
-    static __device__ __forceinline__ int place(int row) { return (ROW % 256 == 0 ? row & 7 : ROW % 128 == 0 ? (row >> 1) & 3 : (row >> 2) & 1) << 1; }
+    // Chunk c of a row lies at position c ^ place(row).  A row-wise read takes one chunk of eight rows at a time, a column-wise one 64 bytes of four rows: of
+    // the 256 bytes that the banks hold side by side, four consecutive rows have a quarter each, and eight rows a position each.
+    static __device__ __forceinline__ int place(int row) {
+        return ROW % 256 == 0 ? (row & 3) << 2 | (row >> 1 & 2) : ROW % 128 == 0 ? (row >> 1 & 1) << 2 | (row >> 1 & 2) : row >> 1 & 2;
+    }
 };
 
 // Sixteen bytes of a row of d channels from channel c on, through a buffer whose end is the last row's: rows beyond are zeros.  Where d is no whole
