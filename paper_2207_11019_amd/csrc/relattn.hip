@@ -35,7 +35,7 @@ struct AttnArgs {
     int32_t m, H, G, pq, pk, d, causal, nb, reach, splits;
     int32_t fold;                         // forward: a block's rows are the queries of all heads that share keys (few queries)
     int64_t ldq, ldk, ldv, ldy;           // elements between positions
-    float scale, scale2;                  // scale2 = scale log2(e)
+    float scale, scale2, inv_scale;       // scale2 = scale log2(e)
     const void *q, *k, *v, *dy;
     void *y, *dq, *dk, *dv;
     const int32_t *len, *start, *map;
@@ -47,7 +47,7 @@ struct AttnArgs {
 
 // WK wavefronts share a block's 128 / WK rows, each with its 32 rows of every tile of the other side.  DMA: tiles go straight from memory to LDS (channels in
 // whole 16-byte chunks, rows on whole dwords); else by way of registers, where a row's last chunk is put in order.
-template <typename T, int DP, int WK_, bool DMA_, bool SMALL = false> struct Ra {
+template <typename T, int DP, int WK_, bool DMA_, int OCC, bool SMALL = false> struct Ra {
     static constexpr int WK = WK_;
     static constexpr bool DMA = DMA_;
     static constexpr int EPC = Mm<T>::EPC, CHUNKS = DP / EPC, KS = DP / (2 * EPC), ES = (int)sizeof(T);
@@ -56,16 +56,31 @@ template <typename T, int DP, int WK_, bool DMA_, bool SMALL = false> struct Ra 
     static constexpr int SUB = BN / (32 * WK);                // 32-row pieces of it that a wavefront takes
     static constexpr int ROW = DP * ES;                       // bytes
     static constexpr int TILE = BN * ROW;
-    static constexpr int STAGES = 2;
-    static constexpr int LDS = 2 * STAGES * TILE;             // tiles of both operands
+    static constexpr int STAGE = 2 * TILE;                    // tiles of both operands
+    // the tile at work, the next on its way, and the one before still in a product where that leaves OCC blocks their room in a CU
+    static constexpr int STAGES = 3 * STAGE <= (OCC == 2 ? 72 : 148) * 1024 ? 3 : 2;
+    static constexpr bool CARRY = STAGES == 3;
+    static constexpr int LDS = STAGES * STAGE;
+    // the wavefronts' diagonals: bfloat16 goes through them in a walk of its own, which needs two stages
+    static constexpr int DIAGONALS = RA_WAVES * 63 * RA_DIAG_PITCH * 4;
+    static constexpr int AREAS = ES == 2 ? 2 * STAGE : LDS, LDS_Q = AREAS + DIAGONALS > LDS ? AREAS + DIAGONALS : LDS;
     static constexpr int PER = BN * CHUNKS / RA_THREADS;      // chunks of a tile a thread brings
     static constexpr int DT = DP / 32;                        // 32-channel pieces of a head
+    static constexpr int NU = 16 / EPC;                       // operands of a column of 32 probabilities
     // Chunk c of a row lies at position c ^ place(row).  A row-wise read takes one chunk of eight rows at a time, a column-wise one 64 bytes of four rows: of
     // the 256 bytes that the banks hold side by side, four consecutive rows have a quarter each, and eight rows a position each.
     static __device__ __forceinline__ int place(int row) {
         return ROW % 256 == 0 ? (row & 3) << 2 | (row >> 1 & 2) : ROW % 128 == 0 ? (row >> 1 & 1) << 2 | (row >> 1 & 2) : row >> 1 & 2;
     }
 };
+
+// Blocks of a CU that a kernel's registers leave room for, and its tiles.  (The tiles of wide heads are small where 64 rows would leave room for one block: forward, 8192 keys
+// of 128 channels, 535 -> RA_FWD_US us.)
+template <typename T, int DP> constexpr int RA_OCC_Q = sizeof(T) == 2 || DP <= 32 ? 2 : 1;
+template <typename T, int DP> constexpr int RA_OCC_KV = DP <= 32 || (sizeof(T) == 2 && DP <= 64) ? 2 : 1;
+template <typename T, int DP, int WK, bool DMA> using RaFwd = Ra<T, DP, WK, DMA, 2, (DP > 64)>;
+template <typename T, int DP, int WK, bool DMA> using RaBwdQ = Ra<T, DP, WK, DMA, RA_OCC_Q<T, DP>, (DP > 64)>;
+template <typename T, int DP, int WK, bool DMA> using RaBwdKv = Ra<T, DP, WK, DMA, RA_OCC_KV<T, DP>>;
 
 // Sixteen bytes of a row of d channels from channel c on, through a buffer whose end is the last row's: rows beyond are zeros.  Where d is no whole
 // number of chunks the last one is taken from the row's end (ra_shift puts it in its place).
@@ -114,7 +129,7 @@ template <typename T, typename R> struct RaTile {
         base += (int64_t)row0 * ld;
         if constexpr (R::DMA) {
             const u32x4_ buf = buffer_words(base, ra_bytes<T>(ld, n, d));
-            unsigned char* to = lds + s * 2 * R::TILE + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 1024;
+            unsigned char* to = lds + s * R::STAGE + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 1024;
 #pragma unroll
             for (int i = 0; i < R::PER; ++i) load_to_lds16(buf, to + i * RA_THREADS * 16, off[i]);
         } else {
@@ -129,7 +144,7 @@ template <typename T, typename R> struct RaTile {
             for (int i = 0; i < R::PER; ++i) {
                 const int at = i * RA_THREADS + (int)threadIdx.x, r = at / R::CHUNKS;
                 const uint4 w = d % R::EPC ? ra_shift<T>(v[i], ((at - r * R::CHUNKS) ^ R::place(r)) * R::EPC, d) : v[i];
-                *reinterpret_cast<uint4*>(lds + s * 2 * R::TILE + at * 16) = w;
+                *reinterpret_cast<uint4*>(lds + s * R::STAGE + at * 16) = w;
             }
         }
     }
@@ -137,41 +152,81 @@ template <typename T, typename R> struct RaTile {
 template <typename R> __device__ __forceinline__ void ra_landed() {
     if constexpr (R::DMA) LPM_WAIT_VM(0);
 }
-// a wavefront's 32 rows as an operand: the lane's row (below `rows`, or zeros), its half of every 2 * EPC channels
+// a wavefront's 32 rows as an operand: the lane's row (`first` elements into a buffer; not there: zeros), its half of every 2 * EPC channels
 template <typename T, typename R> struct RaRows {
     uint4 v[R::KS];
-    __device__ __forceinline__ void load(const T* base, int64_t ld, int64_t row, bool there, int rows, int d, int g) {
-        const auto buf = ra_buffer(base, ld, rows, d);
+    __device__ __forceinline__ void load(const T* base, unsigned bytes, int64_t first, bool there, int d, int g) {
+        const auto buf = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(base), 0, bytes, 0x00020000);
+        const unsigned at = (unsigned)(first * (int64_t)sizeof(T));
 #pragma unroll
         for (int s = 0; s < R::KS; ++s) {
             const int c = (2 * s + g) * R::EPC;
-            v[s] = ra_load(buf, there ? ra_offset<T>(row, ld, c, d) : 0xffffffffu);
+            v[s] = ra_load(buf, there && c < d ? at + ra_offset<T>(0, 0, c, d) : 0xffffffffu);
         }
         if constexpr (!R::DMA) {
 #pragma unroll
             for (int s = 0; s < R::KS; ++s) if (d % R::EPC) v[s] = ra_shift<T>(v[s], (2 * s + g) * R::EPC, d);
         }
     }
+    // row l of `rows` that lie ld elements apart
+    __device__ __forceinline__ void load(const T* base, int64_t ld, int l, int rows, int d, int g) { load(base, ra_bytes<T>(ld, rows, d), l * ld, l < rows, d, g); }
 };
-// rows row .. row + 31 of a tile times such rows: result[tile row][own row]
-template <typename T, typename R>
-__device__ __forceinline__ mm_f16 ra_products(const unsigned char* tile, int row, const RaRows<T, R>& own, int lane) {
-    mm_f16 acc = {};
-    const unsigned char* p = tile + (row + (lane & 31)) * R::ROW;
-    const int at = (lane >> 5) ^ R::place(lane & 31);
+// Where a lane finds its operands in a tile, as byte offsets from its first row: row-wise (its row, a chunk of every step) and column-wise
+template <typename T, typename R> struct RaOffsets {
+    int row[R::KS], col[R::DT];
+    __device__ __forceinline__ explicit RaOffsets(int lane) {
 #pragma unroll
-    for (int s = 0; s < R::KS; ++s) acc = Mm<T>::mul(*reinterpret_cast<const uint4*>(p + (at ^ (2 * s)) * 16), own.v[s], acc);
-    return acc;
-}
-// out[t][channel 32 t + .][own row] += sum over the tile's rows row .. row + 31 of tile[row][channel] w[row][own row], w as a result lies
-template <typename T, typename R>
-__device__ __forceinline__ void ra_mix(const unsigned char* tile, int row, const float (&w)[16], mm_f16 (&out)[R::DT], int lane) {
+        for (int s = 0; s < R::KS; ++s) row[s] = (lane & 31) * R::ROW + (((2 * s + (lane >> 5)) ^ R::place(lane & 31)) * 16);
 #pragma unroll
-    for (int u = 0; u < 16 / R::EPC; ++u) {
-        const uint4 b = Mm<T>::pack(w + u * R::EPC);
-#pragma unroll
-        for (int t = 0; t < R::DT; ++t) out[t] = Mm<T>::mul(Mm<T>::template columns<R>(tile + (row + 2 * R::EPC * u) * R::ROW, t, lane), b, out[t]);
+        for (int t = 0; t < R::DT; ++t) col[t] = Mm<T>::template column<R>(t, lane);
     }
+};
+// A run of N products: the LDS operands read(i) are asked for AHEAD of use(i, operand), and beside(i) is arithmetic that has nothing to do with them, which runs
+// while the matrix cores multiply.  The order is the code's: left to itself the compiler reads an operand, waits for it and multiplies, 130 cycles of
+// latency for 32 of work.  begin() asks for the first operands -- as what stands beside the last products of the run before.
+template <int N> struct RaStream {
+    static constexpr int AHEAD = N < 4 ? N : 4, SLOTS = AHEAD + 1;
+    uint4 f[SLOTS];
+    template <typename F> __device__ __forceinline__ void begin(int k, F&& read) { f[k] = read(k); }
+    template <typename F, typename G, typename L> __device__ __forceinline__ void run(F&& read, G&& use, L&& beside) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (i + AHEAD < N) f[(i + AHEAD) % SLOTS] = read(i + AHEAD);
+            use(i, f[i % SLOTS]);
+            beside(i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+};
+// What stands beside the products of a run of N before the run `next` of operands read(k): its first reads, one beside each of the last products
+template <int N, typename S, typename F> __device__ __forceinline__ auto ra_before(S& next, F& read) {
+    return [&](int i) __attribute__((always_inline)) {
+        const int k = i - (N - S::AHEAD);
+        if (N >= S::AHEAD) { if (k >= 0) next.begin(k, read); }
+        else if (i == 0) {
+#pragma unroll
+            for (int x = 0; x < S::AHEAD; ++x) next.begin(x, read);
+        }
+    };
+}
+template <int N> __device__ __forceinline__ void ra_zero(uint4 (&w)[N]) {
+#pragma unroll
+    for (int x = 0; x < N; ++x) w[x] = make_uint4(0, 0, 0, 0);
+}
+// a lane's 16 values as operands of the next product
+template <typename T, typename R> __device__ __forceinline__ void ra_pack(const mm_f16& v, uint4* w) {
+    float x[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = v[e];
+#pragma unroll
+    for (int u = 0; u < R::NU; ++u) w[u] = Mm<T>::pack(x + u * R::EPC);
+}
+// Row-wise operand s of a tile (`tile` points at its first row); column-wise operand: rows 2 EPC u .., channels 32 t ..
+template <typename T, typename R> __device__ __forceinline__ uint4 ra_row(const unsigned char* tile, const RaOffsets<T, R>& at, int s) {
+    return *reinterpret_cast<const uint4*>(tile + at.row[s]);
+}
+template <typename T, typename R> __device__ __forceinline__ uint4 ra_column(const unsigned char* tile, const RaOffsets<T, R>& at, int u, int t) {
+    return Mm<T>::template columns<R>(tile + 2 * R::EPC * u * R::ROW, at.col[t]);
 }
 // four consecutive channels of a row, n of them there (WHOLE: all)
 template <bool WHOLE, typename T>
@@ -217,8 +272,8 @@ __device__ __forceinline__ void ra_gather(mm_f16 (&out)[R::DT], float* area, int
 }
 
 __device__ __forceinline__ int ra_clamp(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
-__device__ __forceinline__ int ra_keys(const AttnArgs& a, int n) { return a.len ? ra_clamp(a.len[n], 0, a.pk) : a.pk; }
-__device__ __forceinline__ int ra_start(const AttnArgs& a, int n) { return a.start ? ra_clamp(a.start[n], -(1 << 29), 1 << 29) : 0; }
+__device__ __forceinline__ int ra_keys(const AttnArgs& a, int n) { return a.len ? __builtin_amdgcn_readfirstlane(ra_clamp(a.len[n], 0, a.pk)) : a.pk; }
+__device__ __forceinline__ int ra_start(const AttnArgs& a, int n) { return a.start ? __builtin_amdgcn_readfirstlane(ra_clamp(a.start[n], -(1 << 29), 1 << 29)) : 0; }
 __device__ __forceinline__ bool ra_any(bool v) {
 #ifdef __HIP__
     return __builtin_amdgcn_ballot_w64(v) != 0;
@@ -229,22 +284,27 @@ __device__ __forceinline__ bool ra_any(bool v) {
 #endif
 }
 
-// The bias of `heads` heads from h on by distance, lut[head][rel + reach + RA_PAD], in units of log2.  Finite values stay finite (a mask of the type's
-// lowest value leaves a row of such values with equal probabilities, as the formula does).
+// The bias of `heads` heads from h on by distance, lut[head][rel + reach + RA_PAD], over the scale: the sums q . k begin with it.  Finite values stay
+// finite (a mask of the type's lowest value leaves a row of such values with equal probabilities, as the formula does); *huge: some are so large
+// that the differences of scores have to be taken in the order of the formula.
+constexpr float RA_BIG = 3.402823466e38f, RA_HUGE = 1e28f;
 __host__ __device__ inline int ra_lut(int reach) { return 2 * reach + 1 + 2 * RA_PAD; }
 struct RaBias {
     static constexpr int EARLY = 2;        // entries of a thread whose buckets are on their way from the kernel's beginning on
     int id[EARLY];
-    __device__ __forceinline__ int bucket(const AttnArgs& a, int t) const { return ra_clamp(a.map[ra_clamp(t - RA_PAD, 0, 2 * a.reach)], 0, a.nb - 1); }
     __device__ __forceinline__ void begin(const AttnArgs& a) {
 #pragma unroll
         for (int k = 0; k < EARLY; ++k) id[k] = a.table ? a.map[ra_clamp((int)threadIdx.x + k * RA_THREADS - RA_PAD, 0, 2 * a.reach)] : 0;
     }
-    static __device__ __forceinline__ float units(float b) {
-        const float big = 3.402823466e38f;
-        return fabsf(b) <= big ? fminf(fmaxf(b * RA_LOG2E, -big), big) : b;
+    static __device__ __forceinline__ float put(const AttnArgs& a, float b, int* huge) {
+        if (!(fabsf(b) <= RA_BIG)) return b;
+        const float most = a.scale2 > 1.f ? RA_BIG / a.scale2 : RA_BIG;
+        b = fminf(fmaxf(b * a.inv_scale, -most), most);
+        if (fabsf(b) > RA_HUGE) *huge = 1;
+        return b;
     }
-    __device__ __forceinline__ void store(const AttnArgs& a, int h, int heads, float* lut) const {
+    // (between two barriers: nobody reads lut or *huge before the second, and *huge is 0 before the first)
+    __device__ __forceinline__ void store(const AttnArgs& a, int h, int heads, float* lut, int* huge) const {
         const int n = ra_lut(a.reach), first = (int)threadIdx.x;
         for (int hh = 0; hh < heads; ++hh) {
             const float* row = a.table ? a.table + (int64_t)(h + hh) * a.nb : nullptr;
@@ -252,28 +312,37 @@ struct RaBias {
 #pragma unroll
             for (int k = 0; k < EARLY; ++k) b[k] = row ? row[ra_clamp(id[k], 0, a.nb - 1)] : 0.f;
 #pragma unroll
-            for (int k = 0; k < EARLY; ++k) if (first + k * RA_THREADS < n) lut[hh * n + first + k * RA_THREADS] = units(b[k]);
-            for (int t = first + EARLY * RA_THREADS; t < n; t += RA_THREADS) lut[hh * n + t] = row ? units(row[bucket(a, t)]) : 0.f;
+            for (int k = 0; k < EARLY; ++k) if (first + k * RA_THREADS < n) lut[hh * n + first + k * RA_THREADS] = put(a, b[k], huge);
+            for (int t = first + EARLY * RA_THREADS; t < n; t += RA_THREADS)
+                lut[hh * n + t] = row ? put(a, row[ra_clamp(a.map[ra_clamp(t - RA_PAD, 0, 2 * a.reach)], 0, a.nb - 1)], huge) : 0.f;
         }
     }
 };
 // whether all distances relmin .. relmax have one bias
 __device__ __forceinline__ bool ra_far(int reach, int relmin, int relmax) { return relmax <= -reach || relmin >= reach; }
+// (a far piece's one value is at hand: its products wait for no read of the bias)
+template <int DIR> __device__ __forceinline__ mm_f16 ra_bias_of(const float* at, bool far, float end) {
+    mm_f16 v;
+    if (far) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = end;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = at[DIR * ((e & 3) + 8 * (e >> 2))];
+    }
+    return v;
+}
+// Where biases are huge: a score that stands for the distance from the reference `top`, the two subtracted after the score is rounded
+__device__ __forceinline__ float ra_apart(float acc, float scale2, float top) {
+#pragma clang fp contract(off)
+    const float v = acc * scale2;
+    return (v - top) * (1.f / scale2);
+}
 
 __host__ __device__ inline int64_t ra_distances(int reach) { return 2 * (int64_t)reach + 1; }
 
 // Blocks of one head lie on one XCD, one after the other.  Causal: those with the most visible keys first, heads in turn (REVERSE: the last tiles have the
 // most), over as many heads as an XCD has -- all of them, where they do not come in eights.
-// A tile of scores is FAR: one bias for all of it and every pair visible; NEAR: a bias by distance, every pair visible; EDGE: any.
-enum { RA_FAR = 0, RA_NEAR = 1, RA_EDGE = 2 };
-template <int V> struct RaMode { static constexpr int value = V; };
-// f(mode) without a branch inside it, so that the reads of one product run beside the arithmetic of another
-template <typename F> __device__ __forceinline__ void ra_dispatch(bool edge, bool far, F&& f) {
-    if (edge) f(RaMode<RA_EDGE>());
-    else if (far) f(RaMode<RA_FAR>());
-    else f(RaMode<RA_NEAR>());
-}
-
 struct RaBlock { int n, h, tile, split; };
 template <bool REVERSE> __device__ __forceinline__ RaBlock ra_block(int m, int heads, int tiles, int splits, bool causal) {
     const int pairs = m * heads;
@@ -301,10 +370,12 @@ template <bool REVERSE> __device__ __forceinline__ RaBlock ra_block(int m, int h
 
 template <typename T, int DP, int WK, bool DMA>
 __global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
-    typedef Ra<T, DP, WK, DMA> R;
+    typedef RaFwd<T, DP, WK, DMA> R;
     extern __shared__ __attribute__((aligned(16))) unsigned char ra_lds[];
-    float* lut = reinterpret_cast<float*>(ra_lds + R::LDS);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 31, g = lane >> 5, wq = wave / WK, wk = wave % WK;
+    int* huge = reinterpret_cast<int*>(ra_lds + R::LDS);
+    float* lut = reinterpret_cast<float*>(huge + 4);
+    if (threadIdx.x == 0) *huge = 0;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = lane & 31, g = lane >> 5, wq = wave / WK, wk = wave % WK;
     RaBias bias;
     bias.begin(a);
     const int share = a.H / a.G, rows = a.fold ? share * a.pq : a.pq, tiles = (rows + R::BM - 1) / R::BM;
@@ -323,84 +394,115 @@ __global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
     RaTile<T, R> kr, vr;
     kr.place(ra_lds, a.ldk, a.d);
     vr.place(ra_lds + R::TILE, a.ldv, a.d);
-    if (t0 < t1) { kr.load(kb, a.ldk, t0 * R::BN, end, a.d, t0 & 1); vr.load(vb, a.ldv, t0 * R::BN, end, a.d, t0 & 1); }
+    auto load = [&](int t, int stage) __attribute__((always_inline)) {
+        kr.load(kb, a.ldk, t * R::BN, end, a.d, stage);
+        vr.load(vb, a.ldv, t * R::BN, end, a.d, stage);
+    };
+    if (t0 < t1) load(t0, 0);
     RaRows<T, R> qr;
-    if (a.fold)                             // (rows of other heads lie d elements apart: from the sample's first query on)
-        qr.load((const T*)a.q + ((int64_t)n * a.pq + i) * a.ldq + (int64_t)h * a.d, 0, 0, work, 1, a.d, g);
+    if (a.fold)
+        qr.load((const T*)a.q + (int64_t)n * a.pq * a.ldq + (int64_t)h0 * a.d, ra_bytes<T>(a.ldq, a.pq, share * a.d), i * a.ldq + hh * a.d, work, a.d, g);
     else
-        qr.load((const T*)a.q + ((int64_t)n * a.pq + r0) * a.ldq + (int64_t)h * a.d, a.ldq, i - r0, work, min(32, a.pq - r0), a.d, g);
-    bias.store(a, h0, a.fold ? share : 1, lut);
+        qr.load((const T*)a.q + ((int64_t)n * a.pq + r0) * a.ldq + (int64_t)h * a.d, a.ldq, l, min(32, a.pq - r0), a.d, g);
+    const RaOffsets<T, R> at(lane);
+    __syncthreads();
+    bias.store(a, h0, a.fold ? share : 1, lut, huge);
     lut += hh * ra_lut(a.reach);
     mm_f16 o[R::DT] = {};
-    float top = -INFINITY, sum = 0.f;
-    for (int t = t0; t < t1; ++t) {
-        const unsigned char *kt = ra_lds + (t & 1) * 2 * R::TILE, *vt = kt + R::TILE;
-        kr.done(a.d, t & 1);
-        vr.done(a.d, t & 1);
+    float top = -INFINITY, sum = 0.f, before_end = 0.f, behind_end = 0.f;      // (the bias's ends are known behind the first barrier)
+    bool some_huge = false;
+    // A piece's p enters its product while the next piece's is made: `prev` are the values it belongs to, w its operands.  (Before the first piece w is zero, and
+    // prev the first piece's own values.)
+    const unsigned char* prev = nullptr;
+    uint4 w[R::NU] = {};
+    RaStream<R::NU * R::DT> mix;
+    auto values_of = [&](int x) __attribute__((always_inline)) { return ra_column<T, R>(prev, at, x / R::DT, x % R::DT); };
+    auto add = [&](int x, uint4 f) __attribute__((always_inline)) { o[x % R::DT] = Mm<T>::mul(f, w[x / R::DT], o[x % R::DT]); };
+    int stage = 0;
+    auto next_tile = [&](int t) __attribute__((always_inline)) {
+        kr.done(a.d, stage);
+        vr.done(a.d, stage);
         ra_landed<R>();
         __syncthreads();
-        if (t + 1 < t1) { kr.load(kb, a.ldk, (t + 1) * R::BN, end, a.d, (t + 1) & 1); vr.load(vb, a.ldv, (t + 1) * R::BN, end, a.d, (t + 1) & 1); }
-        const int j0 = t * R::BN + wk * 32 * R::SUB;       // the wavefront's keys of the tile
-        if (!work || j0 >= end || (a.causal && j0 > qmax)) continue;
-        const int last = j0 + 32 * R::SUB - 1;
-        const bool far = ra_far(a.reach, j0 - qmax, last - qmin);
-        const float one = lut[RA_PAD + (j0 - qmax >= a.reach ? 2 * a.reach : 0)];
-        // (a bias of the order of the largest numbers swallows the score: only the way that adds the two first gives what the formula gives)
-        const bool edge = last >= keys || (a.causal && last > qmin) || (far && !(fabsf(one) < 1e30f));
-        ra_dispatch(edge, far, [&](auto mode) __attribute__((always_inline)) {
-            constexpr int MODE = decltype(mode)::value;
-            float s[R::SUB][16];
+        if (t + 1 < t1) load(t + 1, stage == R::STAGES - 1 ? 0 : stage + 1);
+    };
+    // the tiles that hold keys for this wavefront: the others of the block may have more
+    const int mine_end = !work ? 0 : a.causal ? min(end, qmax + 1) : end, tw = ra_clamp((mine_end - wk * R::SUB * 32 + R::BN - 1) / R::BN, t0, max(t0, t1));
+    int t = t0;
+    for (; t < tw; ++t, stage = stage == R::STAGES - 1 ? 0 : stage + 1) {
+        next_tile(t);
+        if (t == t0) { before_end = lut[0]; behind_end = lut[2 * a.reach + RA_PAD]; some_huge = __builtin_amdgcn_readfirstlane(*huge); }
+#pragma unroll 1
+        for (int u = 0; u < R::SUB; ++u) {
+            const int at_row = (wk * R::SUB + u) * 32, j0 = t * R::BN + at_row, last = j0 + 31;
+            if (j0 >= mine_end) continue;
+            const unsigned char* kt = ra_lds + stage * R::STAGE + at_row * R::ROW;
+            const bool far = ra_far(a.reach, j0 - qmax, last - qmin), behind = j0 - qmax >= a.reach;
+            const bool edge = last >= keys || (a.causal && last > qmin);
+            if (!prev) prev = kt + R::TILE;
+            constexpr int N = R::NU * R::DT;
+            RaStream<R::KS> products;
+            auto keys_of = [&](int x) __attribute__((always_inline)) { return ra_row<T, R>(kt, at, x); };
+#pragma unroll
+            for (int k = 0; k < products.AHEAD; ++k) products.begin(k, keys_of);
+            mm_f16 s = ra_bias_of<1>(lut + j0 + 4 * g - qpos + a.reach + RA_PAD, far, behind ? behind_end : before_end);
+            products.run(keys_of, [&](int x, uint4 f) __attribute__((always_inline)) { s = Mm<T>::mul(f, qr.v[x], s); }, ra_before<R::KS>(mix, values_of));
+            if (edge) {
+                const int least = (a.causal ? min(keys - 1, qpos) : keys - 1) - j0 - 4 * g;      // the last key that this query sees
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = (e & 3) + 8 * (e >> 2) > least ? -INFINITY : s[e];
+            }
             float mx = -INFINITY;
 #pragma unroll
-            for (int u = 0; u < R::SUB; ++u) {
-                const mm_f16 acc = ra_products<T, R>(kt, wk * 32 * R::SUB + 32 * u, qr, lane);
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[u][e] = acc[e];
-            }
-            if constexpr (MODE != RA_FAR) {
-                const float* near = lut + (far ? (j0 - qmax >= a.reach ? a.reach : -a.reach) : j0 + 4 * g - qpos) + a.reach + RA_PAD;
-                const int least = a.causal ? min(keys - 1, qpos) : keys - 1;      // the last key that this query sees
-#pragma unroll
-                for (int u = 0; u < R::SUB; ++u)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int at = 32 * u + (e & 3) + 8 * (e >> 2);
-                        s[u][e] = fmaf(s[u][e], a.scale2, MODE == RA_EDGE && far ? one : near[at]);
-                        if (MODE == RA_EDGE && j0 + 4 * g + at > least) s[u][e] = -INFINITY;
-                    }
-            }
-#pragma unroll
-            for (int u = 0; u < R::SUB; ++u)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[u][e]);
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            if (MODE == RA_FAR) mx = fmaf(mx, a.scale2, one);
+            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * a.scale2;
             // the reference moves only where a row's maximum has passed it by 2^8 (or it had none): until then p is up to 2^8, which float and
             // bfloat16 hold as exactly as 1
-            if (ra_any(mx > top + 8.f || (top == -INFINITY && mx > top))) {
-                const float to = fmaxf(mx, top), base = to == -INFINITY ? 0.f : to, shrink = exp2_fast(top - base);
-                top = to;
+            const bool move = ra_any(mx > top + 8.f || (top == -INFINITY && mx > top));
+            const float to = move ? fmaxf(mx, top) : top, base = to == -INFINITY ? 0.f : to;
+            float part = 0.f, shift = -base;
+            if (some_huge) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = ra_apart(s[e], a.scale2, base);
+                shift = 0.f;
+            }
+            mix.run(values_of, add, [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+                for (int e = i * 16 / N; e < (i + 1) * 16 / N; ++e) {
+                    s[e] = exp2_fast(fmaf(s[e], a.scale2, shift));
+                    part += s[e];
+                }
+            });
+            if (move) {
+                const float shrink = exp2_fast(top - base);
                 sum *= shrink;
 #pragma unroll
                 for (int c = 0; c < R::DT; ++c)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) o[c][e] *= shrink;
             }
-            const float base = top == -INFINITY ? 0.f : top, rest = one - base;
-            float part = 0.f;
-#pragma unroll
-            for (int u = 0; u < R::SUB; ++u)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    s[u][e] = exp2_fast(MODE == RA_FAR ? fmaf(s[u][e], a.scale2, rest) : s[u][e] - base);
-                    part += s[u][e];
-                }
+            top = to;
             sum += part;
             // (p enters the product in the element type: for bfloat16 an error of 2^-9 of each term, below the rounding of y)
+            ra_pack<T, R>(s, w);
+            prev = kt + R::TILE;
+        }
+        if constexpr (!R::CARRY) {             // (the tile's place is wanted)
+            if (prev) {
 #pragma unroll
-            for (int u = 0; u < R::SUB; ++u) ra_mix<T, R>(vt, wk * 32 * R::SUB + 32 * u, s[u], o, lane);
-        });
+                for (int k = 0; k < mix.AHEAD; ++k) mix.begin(k, values_of);
+                mix.run(values_of, add, [](int) {});
+            }
+            prev = nullptr;
+            ra_zero(w);
+        }
     }
+    if (prev) {
+#pragma unroll
+        for (int k = 0; k < mix.AHEAD; ++k) mix.begin(k, values_of);
+        mix.run(values_of, add, [](int) {});
+    }
+    for (; t < t1; ++t, stage = stage == R::STAGES - 1 ? 0 : stage + 1) next_tile(t);
     sum += __shfl_xor(sum, 32, 64);
     if (WK > 1) {                           // one reference for the wavefronts that share the rows
         float* red = reinterpret_cast<float*>(ra_lds);
@@ -512,7 +614,7 @@ struct RaDiagonals {
         carrying = false;
     }
     // a tile whose key 0 is relmin + 31 positions behind its query 0, not wholly beyond the reach
-    __device__ __forceinline__ void add(const float (&ds)[16], int relmin, float* area, int lane) {
+    __device__ __forceinline__ void add(const mm_f16& ds, int relmin, float* area, int lane) {
         const int l = lane & 31, g = lane >> 5;
         if (!carrying || rel0 != relmin) {
             flush(lane);
@@ -562,12 +664,14 @@ struct RaDiagonals {
 // the sum of a row's ds, which is 0 but for delta's error, corrects it: the sums of tiles beyond the reach afterwards, with those of p beside them,
 // while the tiles within the reach are gone through once more.  (Float: y is as exact as the rest, one walk does it all.)
 template <typename T, int DP, int WK, bool DMA>
-__global__ void __launch_bounds__(RA_THREADS, sizeof(T) == 2 || DP <= 32 ? 2 : 1) relattn_bwd_q(AttnArgs a) {
-    typedef Ra<T, DP, WK, DMA, (DP > 64)> R;
+__global__ void __launch_bounds__(RA_THREADS, (RA_OCC_Q<T, DP>)) relattn_bwd_q(AttnArgs a) {
+    typedef RaBwdQ<T, DP, WK, DMA> R;
     extern __shared__ __attribute__((aligned(16))) unsigned char ra_lds[];
-    float* areas = reinterpret_cast<float*>(ra_lds + R::LDS);
-    float* lut = areas + RA_WAVES * 63 * RA_DIAG_PITCH;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 31, g = lane >> 5, wq = wave / WK, wk = wave % WK;
+    float* areas = reinterpret_cast<float*>(ra_lds + R::AREAS);
+    int* huge = reinterpret_cast<int*>(ra_lds + R::LDS_Q);
+    float* lut = reinterpret_cast<float*>(huge + 4);
+    if (threadIdx.x == 0) *huge = 0;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = lane & 31, g = lane >> 5, wq = wave / WK, wk = wave % WK;
     RaBias bias;
     bias.begin(a);
     float* area = areas + wave * 63 * RA_DIAG_PITCH;
@@ -586,15 +690,19 @@ __global__ void __launch_bounds__(RA_THREADS, sizeof(T) == 2 || DP <= 32 ? 2 : 1
     RaTile<T, R> kr, vr;
     kr.place(ra_lds, a.ldk, a.d);
     vr.place(ra_lds + R::TILE, a.ldv, a.d);
-    if (all > 0) { kr.load(kb, a.ldk, 0, end, a.d, 0); vr.load(vb, a.ldv, 0, end, a.d, 0); }
+    auto load = [&](int t, int stage) __attribute__((always_inline)) {
+        kr.load(kb, a.ldk, t * R::BN, end, a.d, stage);
+        vr.load(vb, a.ldv, t * R::BN, end, a.d, stage);
+    };
+    if (all > 0) load(0, 0);
     const int64_t row = ((int64_t)n * a.H + h) * a.pq + i, first = ((int64_t)n * a.pq + i0) * a.ldy + (int64_t)h * a.d;
     RaRows<T, R> qr, gr;
-    qr.load((const T*)a.q + ((int64_t)n * a.pq + i0) * a.ldq + (int64_t)h * a.d, a.ldq, l, mine, min(32, a.pq - i0), a.d, g);
-    gr.load((const T*)a.dy + first, a.ldy, l, mine, min(32, a.pq - i0), a.d, g);
+    qr.load((const T*)a.q + ((int64_t)n * a.pq + i0) * a.ldq + (int64_t)h * a.d, a.ldq, l, min(32, a.pq - i0), a.d, g);
+    gr.load((const T*)a.dy + first, a.ldy, l, min(32, a.pq - i0), a.d, g);
     float delta = 0.f;
     {
         RaRows<T, R> yr;
-        yr.load((const T*)a.y + first, a.ldy, l, mine, min(32, a.pq - i0), a.d, g);
+        yr.load((const T*)a.y + first, a.ldy, l, min(32, a.pq - i0), a.d, g);
 #pragma unroll
         for (int s = 0; s < R::KS; ++s) {
             T e[R::EPC], f[R::EPC];
@@ -608,101 +716,168 @@ __global__ void __launch_bounds__(RA_THREADS, sizeof(T) == 2 || DP <= 32 ? 2 : 1
     const float2_ stat = mine ? a.stats[row] : float2_{0.f, -INFINITY};
     const bool some = stat.y != -INFINITY;                 // the query sees a key
     const float top = some ? stat.x : 0.f;
+    float shift = stat.y - top;
     const int least = !some ? -1 : a.causal ? min(keys - 1, qpos) : keys - 1;
-    bias.store(a, h, 1, lut);
-    for (int t = lane * 4; t < 63 * RA_DIAG_PITCH; t += 256) *reinterpret_cast<float4*>(area + t) = make_float4(0.f, 0.f, 0.f, 0.f);
+    const RaOffsets<T, R> at(lane);
+    __syncthreads();
+    bias.store(a, h, 1, lut, huge);
+    auto clear = [&]() __attribute__((always_inline)) {
+        for (int t = lane * 4; t < 63 * RA_DIAG_PITCH; t += 256) *reinterpret_cast<float4*>(area + t) = make_float4(0.f, 0.f, 0.f, 0.f);
+    };
+    if (R::ES == 4) clear();
     RaDiagonals dg;
     dg.reach = a.reach;
     dg.line = a.diag ? a.diag + (((int64_t)n * a.H + h) * tiles * RA_WAVES + b.tile * RA_WAVES + wave) * ra_distances(a.reach) : nullptr;
     mm_f16 dq[R::DT] = {};
-    float rowsum = 0.f, far_lo = 0.f, far_hi = 0.f;        // sums of ds over the row, of p beyond the reach on either side
-    // p (dp - delta) of one 32 x 32 tile, and p's sum (of a far one)
-    auto scores = [&](auto mode, const unsigned char* kt, const unsigned char* vt, int at, int j0, bool far, float (&ds)[16], float& psum) __attribute__((always_inline)) {
-        constexpr int MODE = decltype(mode)::value;
-        const mm_f16 s = ra_products<T, R>(kt, at, qr, lane), dp = ra_products<T, R>(vt, at, gr, lane);
-        const float one = lut[RA_PAD + (j0 - qmax >= a.reach ? 2 * a.reach : 0)];
-        const float* near = lut + (far ? 0 : j0 + 4 * g - qpos + a.reach + RA_PAD);
-        psum = 0.f;
+    float rowsum = 0.f, lo = 0.f, hi = 0.f, far_lo = 0.f, far_hi = 0.f;      // sums of ds over the row, of ds and of p beyond the reach on either side
+    float before_end = 0.f, behind_end = 0.f;              // (the bias's ends are known behind the first barrier)
+    bool some_huge = false;
+    // s and dp of the 32 keys from j0 on; beside(i) beside its products
+    auto products = [&](const unsigned char* kt, int j0, bool far, mm_f16& s, mm_f16& dp, auto beside) __attribute__((always_inline)) {
+        RaStream<2 * R::KS> run;
+        auto rows_of = [&](int x) __attribute__((always_inline)) { return ra_row<T, R>(x & 1 ? kt + R::TILE : kt, at, x >> 1); };
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int to = (e & 3) + 8 * (e >> 2);
-            float p = fmaf(s[e], a.scale2, MODE == RA_FAR || (MODE == RA_EDGE && far) ? one : near[to]);
-            p = exp2_fast((p - top) + stat.y);
-            ds[e] = p * (dp[e] - delta);
-            if (MODE == RA_EDGE) {
-                const bool seen = j0 + 4 * g + to <= least;
-                p = seen ? p : 0.f;
-                ds[e] = seen ? ds[e] : 0.f;
-            }
-            if (MODE != RA_NEAR) psum += p;
+        for (int x = 0; x < run.AHEAD; ++x) run.begin(x, rows_of);
+        s = ra_bias_of<1>(lut + j0 + 4 * g - qpos + a.reach + RA_PAD, far, j0 - qmax >= a.reach ? behind_end : before_end);
+        dp = mm_f16{};
+        run.run(rows_of, [&](int x, uint4 f) __attribute__((always_inline)) {
+            if (x & 1) dp = Mm<T>::mul(f, gr.v[x >> 1], dp);
+            else s = Mm<T>::mul(f, qr.v[x >> 1], s);
+        }, beside);
+    };
+    // what stands in the way of p = exp2(scale2 s + shift): pairs that are not visible, and huge biases
+    auto prepare = [&](int j0, mm_f16& s) __attribute__((always_inline)) {
+        if (j0 + 31 >= keys || i0 + 32 > a.pq || (a.causal && j0 + 31 > qmin)) {
+            const int seen = least - j0 - 4 * g;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = (e & 3) + 8 * (e >> 2) <= seen ? s[e] : -INFINITY;
+        }
+        if (some_huge) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = ra_apart(s[e], a.scale2, top);
         }
     };
-    auto edge = [&](int j0) __attribute__((always_inline)) { return j0 + 31 >= keys || i0 + 32 > a.pq || (a.causal && j0 + 31 > qmin); };
-    for (int t = 0; t < all; ++t) {
-        const unsigned char *kt = ra_lds + (t & 1) * 2 * R::TILE, *vt = kt + R::TILE;
-        kr.done(a.d, t & 1);
-        vr.done(a.d, t & 1);
+    // of one pair, p in the place of its score and p (dp - delta) in that of dp
+    auto pair = [&](int e, mm_f16& s, mm_f16& dp) __attribute__((always_inline)) {
+        s[e] = exp2_fast(fmaf(s[e], a.scale2, shift));
+        dp[e] = s[e] * (dp[e] - delta);
+    };
+    // A piece's ds enters its product while the next piece's is made: `prev` are the keys it belongs to, w its operands.  (Before the first piece w is zero,
+    // and prev the first piece's own keys.)
+    const unsigned char* prev = nullptr;
+    uint4 w[R::NU] = {};
+    RaStream<R::NU * R::DT> mix;
+    auto keys_of = [&](int x) __attribute__((always_inline)) { return ra_column<T, R>(prev, at, x / R::DT, x % R::DT); };
+    auto add = [&](int x, uint4 f) __attribute__((always_inline)) { dq[x % R::DT] = Mm<T>::mul(f, w[x / R::DT], dq[x % R::DT]); };
+    int stage = 0;
+    auto next_tile = [&](int t) __attribute__((always_inline)) {
+        kr.done(a.d, stage);
+        vr.done(a.d, stage);
         ra_landed<R>();
         __syncthreads();
-        if (t + 1 < all) { kr.load(kb, a.ldk, (t + 1) * R::BN, end, a.d, (t + 1) & 1); vr.load(vb, a.ldv, (t + 1) * R::BN, end, a.d, (t + 1) & 1); }
+        if (t + 1 < all) load(t + 1, stage == R::STAGES - 1 ? 0 : stage + 1);
+    };
+    // the tiles that hold keys for this wavefront: the others of the block may have more
+    const int mine_end = !work ? 0 : a.causal ? min(end, qmax + 1) : end, tw = ra_clamp((mine_end - wk * R::SUB * 32 + R::BN - 1) / R::BN, 0, all);
+    int t = 0;
+    for (; t < tw; ++t, stage = stage == R::STAGES - 1 ? 0 : stage + 1) {
+        next_tile(t);
+        if (t == 0) {
+            before_end = lut[0];
+            behind_end = lut[2 * a.reach + RA_PAD];
+            some_huge = __builtin_amdgcn_readfirstlane(*huge);
+            if (some_huge) shift = stat.y;
+        }
 #pragma unroll 1
         for (int u = 0; u < R::SUB; ++u) {
-            const int at = (wk * R::SUB + u) * 32, j0 = t * R::BN + at;
-            if (!work || j0 >= end || (a.causal && j0 > qmax)) continue;
-            const bool far = ra_far(a.reach, j0 - qmax, j0 + 31 - qmin), behind = j0 - qmax >= a.reach;
-            ra_dispatch(edge(j0), far, [&](auto mode) __attribute__((always_inline)) {
-                float ds[16], psum, s = 0.f;
-                scores(mode, kt, vt, at, j0, far, ds, psum);
+            const int at_row = (wk * R::SUB + u) * 32, j0 = t * R::BN + at_row;
+            if (j0 >= mine_end) continue;
+            const unsigned char* kt = ra_lds + stage * R::STAGE + at_row * R::ROW;
+            const bool far = ra_far(a.reach, j0 - qmax, j0 + 31 - qmin);
+            if (!prev) prev = kt;
+            constexpr int N = R::NU * R::DT;
+            mm_f16 s, dp;                      // scores and dy . v, then p and ds
+            products(kt, j0, far, s, dp, ra_before<2 * R::KS>(mix, keys_of));
+            prepare(j0, s);
+            float total = 0.f, ps = 0.f;
+            mix.run(keys_of, add, [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s += ds[e];
-                rowsum += s;
-                if (decltype(mode)::value != RA_NEAR) {
-                    dg.hi += far && behind ? s : 0.f;
-                    far_hi += far && behind ? psum : 0.f;
-                    dg.lo += far && !behind ? s : 0.f;
-                    far_lo += far && !behind ? psum : 0.f;
+                for (int e = i * 16 / N; e < (i + 1) * 16 / N; ++e) {
+                    pair(e, s, dp);
+                    total += dp[e];
+                    ps += s[e];
                 }
-                if (R::ES == 4 && dg.line && !far) dg.add(ds, j0 - qmin - 31, area, lane);
-                ra_mix<T, R>(kt, at, ds, dq, lane);
             });
+            rowsum += total;
+            if (far) {
+                const bool behind = j0 - qmax >= a.reach;
+                lo += behind ? 0.f : total;
+                hi += behind ? total : 0.f;
+                far_lo += behind ? 0.f : ps;
+                far_hi += behind ? ps : 0.f;
+            } else if (R::ES == 4 && dg.line) {
+                dg.add(dp, j0 - qmin - 31, area, lane);
+            }
+            ra_pack<T, R>(dp, w);
+            prev = kt;
+        }
+        if constexpr (!R::CARRY) {             // (the tile's place is wanted)
+            if (prev) {
+#pragma unroll
+                for (int k = 0; k < mix.AHEAD; ++k) mix.begin(k, keys_of);
+                mix.run(keys_of, add, [](int) {});
+            }
+            prev = nullptr;
+            ra_zero(w);
         }
     }
+    if (prev) {
+#pragma unroll
+        for (int k = 0; k < mix.AHEAD; ++k) mix.begin(k, keys_of);
+        mix.run(keys_of, add, [](int) {});
+    }
+    for (; t < all; ++t, stage = stage == R::STAGES - 1 ? 0 : stage + 1) next_tile(t);
     if (R::ES == 2 && dg.line) {
         rowsum += __shfl_xor(rowsum, 32, 64);
+        __syncthreads();                    // (the tiles have been read)
         if (WK > 1) {                       // ... over the wavefronts that share the row
-            __syncthreads();
             float* red = reinterpret_cast<float*>(ra_lds);
             if (g == 0) red[wave * 32 + l] = rowsum;
             __syncthreads();
             rowsum = 0.f;
 #pragma unroll
-            for (int w = 0; w < WK; ++w) rowsum += red[(wq * WK + w) * 32 + l];
+            for (int x = 0; x < WK; ++x) rowsum += red[(wq * WK + x) * 32 + l];
+            __syncthreads();
         }
         delta += some ? rowsum : 0.f;
-        dg.lo = fmaf(-rowsum, far_lo, dg.lo);
-        dg.hi = fmaf(-rowsum, far_hi, dg.hi);
+        lo = fmaf(-rowsum, far_lo, lo);
+        hi = fmaf(-rowsum, far_hi, hi);
+        clear();
         // the tiles with distances within the reach of some query of the block
         const int t0 = ra_clamp(block_qmin - a.reach, 0, end) / R::BN, t1 = min(all, ra_clamp(block_qmax + a.reach, 0, end) / R::BN + 1);
-        __syncthreads();                   // (the tiles before have been read)
-        if (t0 < t1) { kr.load(kb, a.ldk, t0 * R::BN, end, a.d, t0 & 1); vr.load(vb, a.ldv, t0 * R::BN, end, a.d, t0 & 1); }
+        if (t0 < t1) load(t0, 0);
         for (int t = t0; t < t1; ++t) {
-            const unsigned char *kt = ra_lds + (t & 1) * 2 * R::TILE, *vt = kt + R::TILE;
-            kr.done(a.d, t & 1);
-            vr.done(a.d, t & 1);
+            const int s2 = (t - t0) & 1;
+            kr.done(a.d, s2);
+            vr.done(a.d, s2);
             ra_landed<R>();
             __syncthreads();
-            if (t + 1 < t1) { kr.load(kb, a.ldk, (t + 1) * R::BN, end, a.d, (t + 1) & 1); vr.load(vb, a.ldv, (t + 1) * R::BN, end, a.d, (t + 1) & 1); }
+            if (t + 1 < t1) load(t + 1, s2 ^ 1);
 #pragma unroll 1
             for (int u = 0; u < R::SUB; ++u) {
-                const int at = (wk * R::SUB + u) * 32, j0 = t * R::BN + at;
+                const int at_row = (wk * R::SUB + u) * 32, j0 = t * R::BN + at_row;
                 if (!work || j0 >= end || (a.causal && j0 > qmax) || ra_far(a.reach, j0 - qmax, j0 + 31 - qmin)) continue;
-                float ds[16], psum;
-                if (edge(j0)) scores(RaMode<RA_EDGE>(), kt, vt, at, j0, false, ds, psum);
-                else scores(RaMode<RA_NEAR>(), kt, vt, at, j0, false, ds, psum);
-                dg.add(ds, j0 - qmin - 31, area, lane);
+                mm_f16 s, dp;
+                products(ra_lds + s2 * R::STAGE + at_row * R::ROW, j0, false, s, dp, [](int) {});
+                prepare(j0, s);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) pair(e, s, dp);
+                dg.add(dp, j0 - qmin - 31, area, lane);
             }
         }
     }
+    dg.lo += lo;
+    dg.hi += hi;
     if (mine && g == 0 && wk == 0) a.delta[row] = delta;
     if (dg.line) dg.finish(lane);
     ra_gather<R>(dq, reinterpret_cast<float*>(ra_lds), wq, wk, lane);
@@ -722,12 +897,14 @@ __global__ void __launch_bounds__(RA_THREADS, sizeof(T) == 2 || DP <= 32 ? 2 : 1
 
 // dk and dv of a block's keys: the queries of every head that shares them, one head after the other
 template <typename T, int DP, int WK, bool DMA>
-__global__ void __launch_bounds__(RA_THREADS, DP <= 32 || (sizeof(T) == 2 && DP <= 64) ? 2 : 1) relattn_bwd_kv(AttnArgs a) {
-    typedef Ra<T, DP, WK, DMA> R;
+__global__ void __launch_bounds__(RA_THREADS, (RA_OCC_KV<T, DP>)) relattn_bwd_kv(AttnArgs a) {
+    typedef RaBwdKv<T, DP, WK, DMA> R;
     extern __shared__ __attribute__((aligned(16))) unsigned char ra_lds[];
-    float* rowvs = reinterpret_cast<float*>(ra_lds + R::LDS);         // two of [3][BN]: top, -log2 sum, delta
-    float* lut = rowvs + 6 * R::BN;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l = lane & 31, g = lane >> 5, wq = wave / WK, wk = wave % WK;
+    float* rowvs = reinterpret_cast<float*>(ra_lds + R::LDS);         // two of [4][BN]: -log2 sum less top, delta, top, -log2 sum
+    int* huge = reinterpret_cast<int*>(rowvs + 8 * R::BN);
+    float* lut = reinterpret_cast<float*>(huge + 4);
+    if (threadIdx.x == 0) *huge = 0;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l = lane & 31, g = lane >> 5, wq = wave / WK, wk = wave % WK;
     RaBias bias;
     bias.begin(a);
     const int tiles = (a.pk + R::BM - 1) / R::BM;
@@ -737,14 +914,29 @@ __global__ void __launch_bounds__(RA_THREADS, DP <= 32 || (sizeof(T) == 2 && DP 
     const int start = ra_start(a, n), keys = ra_keys(a, n);
     const bool work = j0 < keys, mine = j0 + l < keys;
     RaRows<T, R> kr, vr;
-    kr.load((const T*)a.k + ((int64_t)n * a.pk + j0) * a.ldk + (int64_t)hk * a.d, a.ldk, l, mine, min(32, keys - j0), a.d, g);
-    vr.load((const T*)a.v + ((int64_t)n * a.pk + j0) * a.ldv + (int64_t)hk * a.d, a.ldv, l, mine, min(32, keys - j0), a.d, g);
+    kr.load((const T*)a.k + ((int64_t)n * a.pk + j0) * a.ldk + (int64_t)hk * a.d, a.ldk, l, min(32, keys - j0), a.d, g);
+    vr.load((const T*)a.v + ((int64_t)n * a.pk + j0) * a.ldv + (int64_t)hk * a.d, a.ldv, l, min(32, keys - j0), a.d, g);
+    const RaOffsets<T, R> at(lane);
     mm_f16 dk[R::DT] = {}, dv[R::DT] = {};
     const int first = a.causal ? ra_clamp(b.tile * R::BM - start, 0, a.pq) : 0;       // no query before it sees one of the block's keys
     const int t0 = first / R::BN, t1 = b.tile * R::BM < keys ? (a.pq + R::BN - 1) / R::BN : 0;
     RaTile<T, R> qs, gs;
     qs.place(ra_lds, a.ldq, a.d);
     gs.place(ra_lds + R::TILE, a.ldy, a.d);
+    float before_end = 0.f, behind_end = 0.f;              // (the bias's ends are known behind a head's first barrier)
+    bool some_huge = false;
+    // A piece's p and ds enter their products while the next piece's are made: `prev` are the queries they belong to, w the operands.  (Before the first piece w is
+    // zero, and prev the first piece's own queries.)
+    const unsigned char* prev;
+    uint4 w[2 * R::NU];
+    RaStream<2 * R::NU * R::DT> mix;
+    auto columns_of = [&](int x) __attribute__((always_inline)) {
+        return ra_column<T, R>(x < R::NU * R::DT ? prev + R::TILE : prev, at, x / R::DT % R::NU, x % R::DT);
+    };
+    auto add = [&](int x, uint4 f) __attribute__((always_inline)) {
+        if (x < R::NU * R::DT) dv[x % R::DT] = Mm<T>::mul(f, w[x / R::DT], dv[x % R::DT]);
+        else dk[x % R::DT] = Mm<T>::mul(f, w[x / R::DT], dk[x % R::DT]);
+    };
     for (int hh = 0; hh < share; ++hh) {
         const int h = hk * share + hh;
         const T* qb = (const T*)a.q + (int64_t)n * a.pq * a.ldq + (int64_t)h * a.d;
@@ -752,64 +944,104 @@ __global__ void __launch_bounds__(RA_THREADS, DP <= 32 || (sizeof(T) == 2 && DP 
         const int64_t row0 = ((int64_t)n * a.H + h) * a.pq;
         float2_ st = {0.f, -INFINITY};
         float dl = 0.f;
-        auto load = [&](int t) __attribute__((always_inline)) {
-            qs.load(qb, a.ldq, t * R::BN, a.pq, a.d, t & 1);
-            gs.load(gb, a.ldy, t * R::BN, a.pq, a.d, t & 1);
+        auto load = [&](int t, int stage) __attribute__((always_inline)) {
+            qs.load(qb, a.ldq, t * R::BN, a.pq, a.d, stage);
+            gs.load(gb, a.ldy, t * R::BN, a.pq, a.d, stage);
             const int i = min(t * R::BN + min((int)threadIdx.x, R::BN - 1), a.pq - 1);      // (rows beyond the last are masked)
             st = a.stats[row0 + i];
             dl = a.delta[row0 + i];
         };
         __syncthreads();                                   // (the tiles and the bias of the head before have been read)
-        if (t0 < t1) load(t0);
-        bias.store(a, h, 1, lut);
-        for (int t = t0; t < t1; ++t) {
-            const unsigned char *qt = ra_lds + (t & 1) * 2 * R::TILE, *gt = qt + R::TILE;
-            float* rowv = rowvs + (t & 1) * 3 * R::BN;
-            qs.done(a.d, t & 1);
-            gs.done(a.d, t & 1);
+        if (t0 < t1) load(t0, 0);
+        bias.store(a, h, 1, lut, huge);
+        prev = nullptr;
+        ra_zero(w);
+        int stage = 0;
+        for (int t = t0; t < t1; ++t, stage = stage == R::STAGES - 1 ? 0 : stage + 1) {
+            float* rowv = rowvs + (t & 1) * 4 * R::BN;
+            qs.done(a.d, stage);
+            gs.done(a.d, stage);
             if ((int)threadIdx.x < R::BN) {
-                rowv[threadIdx.x] = st.y == -INFINITY ? 0.f : st.x;
-                rowv[R::BN + threadIdx.x] = st.y;
-                rowv[2 * R::BN + threadIdx.x] = dl;
+                const float tp = st.y == -INFINITY ? 0.f : st.x;
+                rowv[threadIdx.x] = st.y - tp;
+                rowv[R::BN + threadIdx.x] = dl;
+                rowv[2 * R::BN + threadIdx.x] = tp;
+                rowv[3 * R::BN + threadIdx.x] = st.y;
             }
             ra_landed<R>();
             __syncthreads();
-            if (t + 1 < t1) load(t + 1);
+            if (t + 1 < t1) load(t + 1, stage == R::STAGES - 1 ? 0 : stage + 1);
+            if (t == t0) { before_end = lut[0]; behind_end = lut[2 * a.reach + RA_PAD]; some_huge = __builtin_amdgcn_readfirstlane(*huge); }
 #pragma unroll 1
             for (int u = 0; u < R::SUB; ++u) {
-                const int at = (wk * R::SUB + u) * 32, i0 = t * R::BN + at, qmin = i0 + start, qmax = min(i0 + 31, a.pq - 1) + start;
-                if (!work || i0 >= a.pq || (a.causal && j0 > qmax)) continue;
-                const bool far = ra_far(a.reach, j0 - i0 - start - 31, j0 + 31 - qmin);
+                const int at_row = (wk * R::SUB + u) * 32, i0 = t * R::BN + at_row, qmin = i0 + start, qmax = min(i0 + 31, a.pq - 1) + start;
+                if (!work || i0 >= a.pq || (a.causal && j0 > qmax)) continue;      // (before the first piece, or behind the last)
+                const unsigned char *qt = ra_lds + stage * R::STAGE + at_row * R::ROW, *gt = qt + R::TILE;
+                const float* rv = rowv + at_row + 4 * g;
+                const int relmin = j0 - i0 - start - 31;
+                const bool far = ra_far(a.reach, relmin, j0 + 31 - qmin), behind = relmin >= a.reach;
                 const bool edge = j0 + 32 > keys || i0 + 32 > a.pq || (a.causal && j0 + 31 > qmin);
-                ra_dispatch(edge, far, [&](auto mode) __attribute__((always_inline)) {
-                    constexpr int MODE = decltype(mode)::value;
-                    const mm_f16 s = ra_products<T, R>(qt, at, kr, lane), dp = ra_products<T, R>(gt, at, vr, lane);
-                    const float one = lut[RA_PAD + (j0 - i0 - start - 31 >= a.reach ? 2 * a.reach : 0)];
-                    const float* near = lut + (far ? 64 : j0 + l - i0 - start - 4 * g + a.reach + RA_PAD);
-                    const int from = a.causal ? j0 + l - start : 0;      // the first query that sees this key
-                    float p[16], ds[16];
+                if (!prev) prev = qt;
+                constexpr int N = 2 * R::NU * R::DT;
+                RaStream<2 * R::KS> products;
+                auto rows_of = [&](int x) __attribute__((always_inline)) { return ra_row<T, R>(x & 1 ? gt : qt, at, x >> 1); };
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const float* rv = rowv + at + 8 * c + 4 * g;
-                        const float4 tp = *reinterpret_cast<const float4*>(rv), ls = *reinterpret_cast<const float4*>(rv + R::BN), de = *reinterpret_cast<const float4*>(rv + 2 * R::BN);
-                        const float tops[4] = {tp.x, tp.y, tp.z, tp.w}, logs[4] = {ls.x, ls.y, ls.z, ls.w}, deltas[4] = {de.x, de.y, de.z, de.w};
+                for (int x = 0; x < products.AHEAD; ++x) products.begin(x, rows_of);
+                mm_f16 s = ra_bias_of<-1>(lut + j0 + l - i0 - start - 4 * g + a.reach + RA_PAD, far, behind ? behind_end : before_end), dp = {};
+                products.run(rows_of, [&](int x, uint4 f) __attribute__((always_inline)) {
+                    if (x & 1) dp = Mm<T>::mul(f, vr.v[x >> 1], dp);
+                    else s = Mm<T>::mul(f, kr.v[x >> 1], s);
+                }, ra_before<2 * R::KS>(mix, columns_of));
+                if (edge) {
+                    // queries of the piece that see this key
+                    const int from = (a.causal ? max(j0 + l - start, 0) : 0) - i0 - 4 * g, to = mine ? a.pq - i0 - 4 * g : 0;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const int e = 4 * c + k, i = i0 + 4 * g + k + 8 * c;
-                            const float v = fmaf(s[e], a.scale2, MODE == RA_FAR || (MODE == RA_EDGE && far) ? one : near[-(k + 8 * c)]);
-                            p[e] = exp2_fast((v - tops[k]) + logs[k]);
-                            ds[e] = p[e] * (dp[e] - deltas[k]);
-                            if (MODE == RA_EDGE) {
-                                const bool seen = mine && i < a.pq && i >= from && logs[k] != -INFINITY;
-                                p[e] = seen ? p[e] : 0.f;
-                                ds[e] = seen ? ds[e] : 0.f;
-                            }
-                        }
+                    for (int e = 0; e < 16; ++e) {
+                        const int i = (e & 3) + 8 * (e >> 2);
+                        s[e] = (i < to) & (i >= from) ? s[e] : -INFINITY;
                     }
-                    ra_mix<T, R>(gt, at, p, dv, lane);
-                    ra_mix<T, R>(qt, at, ds, dk, lane);
+                }
+                const float* shift_at = rv;
+                if (some_huge) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[e] = ra_apart(s[e], a.scale2, rv[2 * R::BN + (e & 3) + 8 * (e >> 2)]);
+                    shift_at = rv + 3 * R::BN;
+                }
+                float4 shifts[2], deltas[2];       // of four rows, and of the next four
+                auto rows4 = [&](int c) __attribute__((always_inline)) {
+                    shifts[c & 1] = *reinterpret_cast<const float4*>(shift_at + 8 * c);
+                    deltas[c & 1] = *reinterpret_cast<const float4*>(rv + R::BN + 8 * c);
+                };
+                rows4(0);
+                mix.run(columns_of, add, [&](int x) __attribute__((always_inline)) {
+#pragma unroll
+                    for (int e = x * 16 / N; e < (x + 1) * 16 / N; ++e) {
+                        const int c = e >> 2;
+                        if (e % 4 == 0 && c < 3) rows4(c + 1);
+                        const float4 sh = shifts[c & 1], de = deltas[c & 1];
+                        const float delta = e % 4 == 0 ? de.x : e % 4 == 1 ? de.y : e % 4 == 2 ? de.z : de.w;
+                        s[e] = exp2_fast(fmaf(s[e], a.scale2, e % 4 == 0 ? sh.x : e % 4 == 1 ? sh.y : e % 4 == 2 ? sh.z : sh.w));
+                        dp[e] = s[e] * (dp[e] - delta);
+                    }
                 });
+                ra_pack<T, R>(s, w);
+                ra_pack<T, R>(dp, w + R::NU);
+                prev = qt;
             }
+            if constexpr (!R::CARRY) {             // (the tile's place is wanted)
+                if (prev) {
+#pragma unroll
+                    for (int k = 0; k < mix.AHEAD; ++k) mix.begin(k, columns_of);
+                    mix.run(columns_of, add, [](int) {});
+                }
+                prev = nullptr;
+                ra_zero(w);
+            }
+        }
+        if (prev) {
+#pragma unroll
+            for (int k = 0; k < mix.AHEAD; ++k) mix.begin(k, columns_of);
+            mix.run(columns_of, add, [](int) {});
         }
     }
     ra_gather<R>(dk, reinterpret_cast<float*>(ra_lds), wq, wk, lane);
@@ -917,24 +1149,24 @@ template <typename K> static hipError_t ra_launch(K kernel, DeviceSet& done, int
     return hipGetLastError();
 }
 template <typename T, int DP, int WK, bool DMA> static hipError_t ra_forward(const AttnArgs& a, hipStream_t st) {
-    typedef Ra<T, DP, WK, DMA> R;
+    typedef RaFwd<T, DP, WK, DMA> R;
     static DeviceSet done;
     const int share = a.H / a.G, rows = a.fold ? share * a.pq : a.pq;
     return ra_launch(relattn_fwd<T, DP, WK, DMA>, done, (int64_t)a.m * (a.fold ? a.G : a.H) * ((rows + R::BM - 1) / R::BM) * a.splits,
-                     R::LDS + (size_t)(a.fold ? share : 1) * ra_lut(a.reach) * 4, a, st);
+                     R::LDS + 16 + (size_t)(a.fold ? share : 1) * ra_lut(a.reach) * 4, a, st);
 }
 template <typename T, int DP, int WK, bool DMA> static hipError_t ra_backward_q(const AttnArgs& a, hipStream_t st) {
-    typedef Ra<T, DP, WK, DMA, (DP > 64)> R;
+    typedef RaBwdQ<T, DP, WK, DMA> R;
     static DeviceSet done;
-    static_assert(R::LDS + RA_WAVES * 63 * RA_DIAG_PITCH * 4 + (2 * RA_MAX_REACH + 1 + 2 * RA_PAD) * 4 <= 160 * 1024, "the tiles, diagonals and bias fit");
+    static_assert(R::LDS_Q + 16 + (2 * RA_MAX_REACH + 1 + 2 * RA_PAD) * 4 <= 160 * 1024, "the tiles, diagonals and bias fit");
     static_assert(WK == 1 || 128 / WK / 32 * WK * R::DT * 4096 <= R::LDS, "the sums of wavefronts that share rows fit over the tiles");
     return ra_launch(relattn_bwd_q<T, DP, WK, DMA>, done, (int64_t)a.m * a.H * ((a.pq + R::BM - 1) / R::BM),
-                     R::LDS + RA_WAVES * 63 * RA_DIAG_PITCH * 4 + (size_t)ra_lut(a.reach) * 4, a, st);
+                     R::LDS_Q + 16 + (size_t)ra_lut(a.reach) * 4, a, st);
 }
 template <typename T, int DP, int WK, bool DMA> static hipError_t ra_backward_kv(const AttnArgs& a, hipStream_t st) {
-    typedef Ra<T, DP, WK, DMA> R;
+    typedef RaBwdKv<T, DP, WK, DMA> R;
     static DeviceSet done;
-    return ra_launch(relattn_bwd_kv<T, DP, WK, DMA>, done, (int64_t)a.m * a.G * ((a.pk + R::BM - 1) / R::BM), R::LDS + (6 * R::BN + (size_t)ra_lut(a.reach)) * 4, a, st);
+    return ra_launch(relattn_bwd_kv<T, DP, WK, DMA>, done, (int64_t)a.m * a.G * ((a.pk + R::BM - 1) / R::BM), R::LDS + (8 * R::BN + 4 + (size_t)ra_lut(a.reach)) * 4, a, st);
 }
 // Tiles straight to LDS: channels in whole chunks, every row of both operands on a whole dword
 static bool ra_dma(int32_t dtype, int d, const void* p, int64_t ldp, const void* q, int64_t ldq) {
@@ -981,7 +1213,7 @@ static AttnArgs ra_args(const lpm_attn_geom& g, const void* q, const void* k, co
     a.m = g.m; a.H = g.heads; a.G = g.kv_heads; a.pq = g.pq; a.pk = g.pk; a.d = g.d; a.causal = g.causal != 0;
     a.nb = g.n_buckets; a.reach = g.reach; a.splits = 1;
     a.ldq = g.ldq; a.ldk = g.ldk; a.ldv = g.ldv; a.ldy = g.ldy;
-    a.scale = g.scale; a.scale2 = g.scale * RA_LOG2E;
+    a.scale = g.scale; a.scale2 = g.scale * RA_LOG2E; a.inv_scale = 1.f / g.scale;
     a.q = q; a.k = k; a.v = v;
     a.len = len; a.start = start; a.map = map; a.table = table;
     return a;
