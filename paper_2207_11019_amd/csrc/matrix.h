@@ -28,6 +28,13 @@ template <> struct Mm<bf16_t> {
     static __device__ __forceinline__ uint4 pack(const float* v) {
         return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
     }
+    static __device__ __forceinline__ uint4 scale(uint4 v, float f) {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        uint32_t r[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) r[k] = pack_bf16x2(__uint_as_float(w[k] << 16) * f, __uint_as_float(w[k] & 0xffff0000u) * f);
+        return make_uint4(r[0], r[1], r[2], r[3]);
+    }
     // The LDS transpose read: lane i of 16 receives element i % 4 of the four-element pieces that lanes 4j + i/4 point at, j = 0 .. 3.
     static __device__ LPM_MM_INLINE uint2 read4(const unsigned char* p) {
 #ifdef __HIP__
@@ -67,6 +74,10 @@ template <> struct Mm<float> {
     }
     static __device__ __forceinline__ uint4 pack(const float* v) {
         return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    }
+    static __device__ __forceinline__ uint4 scale(uint4 v, float f) {
+        return make_uint4(__float_as_uint(__uint_as_float(v.x) * f), __float_as_uint(__uint_as_float(v.y) * f), __float_as_uint(__uint_as_float(v.z) * f),
+                          __float_as_uint(__uint_as_float(v.w) * f));
     }
     // ... the rows of half g: 4 g + (0 .. 3), whose places differ from the first one's by a constant in the chunk's bits
     template <typename R> static __device__ __forceinline__ int column(int t, int lane) {

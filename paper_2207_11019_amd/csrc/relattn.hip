@@ -181,6 +181,9 @@ template <typename T, typename R> struct RaOffsets {
         for (int t = 0; t < R::DT; ++t) col[t] = Mm<T>::template column<R>(t, lane);
     }
 };
+// Pins a value to the place where it is made (the compiler would sink arithmetic that stands beside products to where its result is used)
+__device__ __forceinline__ void ra_here(float& v) { asm volatile("" : "+v"(v)); }
+
 // A run of N products: the LDS operands read(i) are asked for AHEAD of use(i, operand), and beside(i) is arithmetic that has nothing to do with them, which runs
 // while the matrix cores multiply.  The order is the code's: left to itself the compiler reads an operand, waits for it and multiplies, 130 cycles of
 // latency for 32 of work.  begin() asks for the first operands -- as what stands beside the last products of the run before.
@@ -455,11 +458,23 @@ __global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
             float mx = -INFINITY;
 #pragma unroll
             for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * a.scale2;
+            mx *= a.scale2;
             // the reference moves only where a row's maximum has passed it by 2^8 (or it had none): until then p is up to 2^8, which float and
             // bfloat16 hold as exactly as 1
             const bool move = ra_any(mx > top + 8.f || (top == -INFINITY && mx > top));
-            const float to = move ? fmaxf(mx, top) : top, base = to == -INFINITY ? 0.f : to;
+            float to = top;
+            if (move) {
+                to = fmaxf(fmaxf(mx, __shfl_xor(mx, 32, 64)), top);
+                const float shrink = exp2_fast(top - (to == -INFINITY ? 0.f : to));
+                sum *= shrink;
+#pragma unroll
+                for (int c = 0; c < R::DT; ++c)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) o[c][e] *= shrink;
+#pragma unroll
+                for (int x = 0; x < R::NU; ++x) w[x] = Mm<T>::scale(w[x], shrink);
+            }
+            const float base = to == -INFINITY ? 0.f : to;
             float part = 0.f, shift = -base;
             if (some_huge) {
 #pragma unroll
@@ -469,18 +484,12 @@ __global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
             mix.run(values_of, add, [&](int i) __attribute__((always_inline)) {
 #pragma unroll
                 for (int e = i * 16 / N; e < (i + 1) * 16 / N; ++e) {
-                    s[e] = exp2_fast(fmaf(s[e], a.scale2, shift));
-                    part += s[e];
+                    float p = exp2_fast(fmaf(s[e], a.scale2, shift));
+                    ra_here(p);
+                    s[e] = p;
+                    part += p;
                 }
             });
-            if (move) {
-                const float shrink = exp2_fast(top - base);
-                sum *= shrink;
-#pragma unroll
-                for (int c = 0; c < R::DT; ++c)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) o[c][e] *= shrink;
-            }
             top = to;
             sum += part;
             // (p enters the product in the element type: for bfloat16 an error of 2^-9 of each term, below the rounding of y)
@@ -759,8 +768,11 @@ __global__ void __launch_bounds__(RA_THREADS, (RA_OCC_Q<T, DP>)) relattn_bwd_q(A
     };
     // of one pair, p in the place of its score and p (dp - delta) in that of dp
     auto pair = [&](int e, mm_f16& s, mm_f16& dp) __attribute__((always_inline)) {
-        s[e] = exp2_fast(fmaf(s[e], a.scale2, shift));
-        dp[e] = s[e] * (dp[e] - delta);
+        float p = exp2_fast(fmaf(s[e], a.scale2, shift)), ds = p * (dp[e] - delta);
+        ra_here(p);
+        ra_here(ds);
+        s[e] = p;
+        dp[e] = ds;
     };
     // A piece's ds enters its product while the next piece's is made: `prev` are the keys it belongs to, w its operands.  (Before the first piece w is zero,
     // and prev the first piece's own keys.)
@@ -809,15 +821,12 @@ __global__ void __launch_bounds__(RA_THREADS, (RA_OCC_Q<T, DP>)) relattn_bwd_q(A
                 }
             });
             rowsum += total;
-            if (far) {
-                const bool behind = j0 - qmax >= a.reach;
-                lo += behind ? 0.f : total;
-                hi += behind ? total : 0.f;
-                far_lo += behind ? 0.f : ps;
-                far_hi += behind ? ps : 0.f;
-            } else if (R::ES == 4 && dg.line) {
-                dg.add(dp, j0 - qmin - 31, area, lane);
-            }
+            const float before = far && j0 - qmax < a.reach ? 1.f : 0.f, behind = far && j0 - qmax >= a.reach ? 1.f : 0.f;
+            lo = fmaf(before, total, lo);
+            hi = fmaf(behind, total, hi);
+            far_lo = fmaf(before, ps, far_lo);
+            far_hi = fmaf(behind, ps, far_hi);
+            if (R::ES == 4 && dg.line && !far) dg.add(dp, j0 - qmin - 31, area, lane);
             ra_pack<T, R>(dp, w);
             prev = kt;
         }
@@ -998,7 +1007,7 @@ __global__ void __launch_bounds__(RA_THREADS, (RA_OCC_KV<T, DP>)) relattn_bwd_kv
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const int i = (e & 3) + 8 * (e >> 2);
-                        s[e] = (i < to) & (i >= from) ? s[e] : -INFINITY;
+                        s[e] = i < to && i >= from ? s[e] : -INFINITY;
                     }
                 }
                 const float* shift_at = rv;
@@ -1020,8 +1029,11 @@ __global__ void __launch_bounds__(RA_THREADS, (RA_OCC_KV<T, DP>)) relattn_bwd_kv
                         if (e % 4 == 0 && c < 3) rows4(c + 1);
                         const float4 sh = shifts[c & 1], de = deltas[c & 1];
                         const float delta = e % 4 == 0 ? de.x : e % 4 == 1 ? de.y : e % 4 == 2 ? de.z : de.w;
-                        s[e] = exp2_fast(fmaf(s[e], a.scale2, e % 4 == 0 ? sh.x : e % 4 == 1 ? sh.y : e % 4 == 2 ? sh.z : sh.w));
-                        dp[e] = s[e] * (dp[e] - delta);
+                        float p = exp2_fast(fmaf(s[e], a.scale2, e % 4 == 0 ? sh.x : e % 4 == 1 ? sh.y : e % 4 == 2 ? sh.z : sh.w)), ds = p * (dp[e] - delta);
+                        ra_here(p);
+                        ra_here(ds);
+                        s[e] = p;
+                        dp[e] = ds;
                     }
                 });
                 ra_pack<T, R>(s, w);
