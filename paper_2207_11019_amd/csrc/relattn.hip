@@ -66,6 +66,7 @@ template <typename T, int DP, int WK_, bool DMA_, int OCC, bool SMALL = false> s
     static constexpr int AREAS = ES == 2 ? 2 * STAGE : LDS, LDS_Q = AREAS + DIAGONALS > LDS ? AREAS + DIAGONALS : LDS;
     static constexpr int PER = BN * CHUNKS / RA_THREADS;      // chunks of a tile a thread brings
     static constexpr int DT = DP / 32;                        // 32-channel pieces of a head
+    static constexpr int AHEAD = DMA ? 6 : 4;                 // operands of a product on their way (8192 keys, dk and dv, 6 against 4: 847 -> 819 us)
     static constexpr int NU = 16 / EPC;                       // operands of a column of 32 probabilities
     // Chunk c of a row lies at position c ^ place(row).  A row-wise read takes one chunk of eight rows at a time, a column-wise one 64 bytes of four rows: of
     // the 256 bytes that the banks hold side by side, four consecutive rows have a quarter each, and eight rows a position each.
@@ -187,8 +188,8 @@ __device__ __forceinline__ void ra_here(float& v) { asm volatile("" : "+v"(v)); 
 // A run of N products: the LDS operands read(i) are asked for AHEAD of use(i, operand), and beside(i) is arithmetic that has nothing to do with them, which runs
 // while the matrix cores multiply.  The order is the code's: left to itself the compiler reads an operand, waits for it and multiplies, 130 cycles of
 // latency for 32 of work.  begin() asks for the first operands -- as what stands beside the last products of the run before.
-template <int N> struct RaStream {
-    static constexpr int AHEAD = N < 4 ? N : 4, SLOTS = AHEAD + 1;
+template <int N, int MOST> struct RaStream {
+    static constexpr int AHEAD = N < MOST ? N : MOST, SLOTS = AHEAD + 1;
     uint4 f[SLOTS];
     template <typename F> __device__ __forceinline__ void begin(int k, F&& read) { f[k] = read(k); }
     template <typename F, typename G, typename L> __device__ __forceinline__ void run(F&& read, G&& use, L&& beside) {
@@ -418,7 +419,7 @@ __global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
     // prev the first piece's own values.)
     const unsigned char* prev = nullptr;
     uint4 w[R::NU] = {};
-    RaStream<R::NU * R::DT> mix;
+    RaStream<R::NU * R::DT, R::AHEAD> mix;
     auto values_of = [&](int x) __attribute__((always_inline)) { return ra_column<T, R>(prev, at, x / R::DT, x % R::DT); };
     auto add = [&](int x, uint4 f) __attribute__((always_inline)) { o[x % R::DT] = Mm<T>::mul(f, w[x / R::DT], o[x % R::DT]); };
     int stage = 0;
@@ -444,7 +445,7 @@ __global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
             const bool edge = last >= keys || (a.causal && last > qmin);
             if (!prev) prev = kt + R::TILE;
             constexpr int N = R::NU * R::DT;
-            RaStream<R::KS> products;
+            RaStream<R::KS, R::AHEAD> products;
             auto keys_of = [&](int x) __attribute__((always_inline)) { return ra_row<T, R>(kt, at, x); };
 #pragma unroll
             for (int k = 0; k < products.AHEAD; ++k) products.begin(k, keys_of);
@@ -743,7 +744,7 @@ __global__ void __launch_bounds__(RA_THREADS, (RA_OCC_Q<T, DP>)) relattn_bwd_q(A
     bool some_huge = false;
     // s and dp of the 32 keys from j0 on; beside(i) beside its products
     auto products = [&](const unsigned char* kt, int j0, bool far, mm_f16& s, mm_f16& dp, auto beside) __attribute__((always_inline)) {
-        RaStream<2 * R::KS> run;
+        RaStream<2 * R::KS, R::AHEAD> run;
         auto rows_of = [&](int x) __attribute__((always_inline)) { return ra_row<T, R>(x & 1 ? kt + R::TILE : kt, at, x >> 1); };
 #pragma unroll
         for (int x = 0; x < run.AHEAD; ++x) run.begin(x, rows_of);
@@ -778,7 +779,7 @@ __global__ void __launch_bounds__(RA_THREADS, (RA_OCC_Q<T, DP>)) relattn_bwd_q(A
     // and prev the first piece's own keys.)
     const unsigned char* prev = nullptr;
     uint4 w[R::NU] = {};
-    RaStream<R::NU * R::DT> mix;
+    RaStream<R::NU * R::DT, R::AHEAD> mix;
     auto keys_of = [&](int x) __attribute__((always_inline)) { return ra_column<T, R>(prev, at, x / R::DT, x % R::DT); };
     auto add = [&](int x, uint4 f) __attribute__((always_inline)) { dq[x % R::DT] = Mm<T>::mul(f, w[x / R::DT], dq[x % R::DT]); };
     int stage = 0;
@@ -938,7 +939,7 @@ __global__ void __launch_bounds__(RA_THREADS, (RA_OCC_KV<T, DP>)) relattn_bwd_kv
     // zero, and prev the first piece's own queries.)
     const unsigned char* prev;
     uint4 w[2 * R::NU];
-    RaStream<2 * R::NU * R::DT> mix;
+    RaStream<2 * R::NU * R::DT, R::AHEAD> mix;
     auto columns_of = [&](int x) __attribute__((always_inline)) {
         return ra_column<T, R>(x < R::NU * R::DT ? prev + R::TILE : prev, at, x / R::DT % R::NU, x % R::DT);
     };
@@ -992,7 +993,7 @@ __global__ void __launch_bounds__(RA_THREADS, (RA_OCC_KV<T, DP>)) relattn_bwd_kv
                 const bool edge = j0 + 32 > keys || i0 + 32 > a.pq || (a.causal && j0 + 31 > qmin);
                 if (!prev) prev = qt;
                 constexpr int N = 2 * R::NU * R::DT;
-                RaStream<2 * R::KS> products;
+                RaStream<2 * R::KS, R::AHEAD> products;
                 auto rows_of = [&](int x) __attribute__((always_inline)) { return ra_row<T, R>(x & 1 ? gt : qt, at, x >> 1); };
 #pragma unroll
                 for (int x = 0; x < products.AHEAD; ++x) products.begin(x, rows_of);
@@ -1095,7 +1096,7 @@ __global__ void __launch_bounds__(RA_THREADS) relattn_buckets(const float* __res
                                                               float* __restrict__ dtable, int accumulate) {
     extern __shared__ __attribute__((aligned(16))) float ra_sums[];
     int* ids = reinterpret_cast<int*>(ra_sums + nd);
-    const int h = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int h = blockIdx.x;
     for (int c = threadIdx.x; c < nd; c += RA_THREADS) {
         float v[RA_SHARES], s = 0.f;
         ids[c] = ra_clamp(map[c], 0, nb - 1);
@@ -1106,24 +1107,33 @@ __global__ void __launch_bounds__(RA_THREADS) relattn_buckets(const float* __res
         ra_sums[c] = s;
     }
     __syncthreads();
-    for (int b = wave; b < nb; b += RA_WAVES) {
+    // eight lanes a bucket
+    const int part = threadIdx.x & 7;
+    for (int b0 = 0; b0 < nb; b0 += RA_THREADS / 8) {
+        const int b = b0 + (int)(threadIdx.x >> 3);
         float s = 0.f;
-        for (int c = lane; c < nd; c += 64) s += ids[c] == b ? ra_sums[c] : 0.f;
+        for (int c = part; c < nd; c += 8) s += ids[c] == b ? ra_sums[c] : 0.f;
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
-        if (lane == 0) dtable[(int64_t)h * nb + b] = accumulate ? dtable[(int64_t)h * nb + b] + s : s;
+        for (int o = 1; o < 8; o <<= 1) s += __shfl_xor(s, o, 64);
+        if (part == 0 && b < nb) dtable[(int64_t)h * nb + b] = accumulate ? dtable[(int64_t)h * nb + b] + s : s;
     }
 }
 
 static size_t ra_up(size_t b) { return (b + 255) & ~(size_t)255; }
 // Wavefronts that share rows (and walk the other side's tiles together): where blocks of 128 rows are too few to give every CU two.
 // (As many as the tiles leave room for in LDS.)
-template <typename T, int DP> constexpr int ra_wide() { return sizeof(T) == 2 ? (DP <= 64 ? 4 : 2) : DP <= 64 ? 2 : 1; }
+template <typename T, int DP> constexpr int ra_wide() { return sizeof(T) == 2 ? (DP <= 64 ? 4 : 2) : DP <= 32 ? 4 : DP <= 64 ? 2 : 1; }
 static int ra_dp(int d, bool dma) { return d <= 32 && dma ? 32 : d <= 64 ? 64 : d <= 96 && dma ? 96 : 128; }
-static int ra_wide_of(int32_t dtype, int dp) { return dtype == LPM_BF16 ? (dp <= 64 ? 4 : 2) : dp <= 64 ? 2 : 1; }
+static int ra_wide_of(int32_t dtype, int dp) { return dtype == LPM_BF16 ? (dp <= 64 ? 4 : 2) : dp <= 32 ? 4 : dp <= 64 ? 2 : 1; }
 static bool ra_shared(int64_t blocks) { return blocks <= 256; }
-// (rows of a block do not depend on whether tiles go straight to LDS: scratch is sized without the operands)
-static int ra_bm(int32_t dtype, int d, int64_t pairs, int rows) { return ra_shared(pairs * ((rows + 127) / 128)) ? 128 / ra_wide_of(dtype, ra_dp(d, false)) : 128; }
+static int ra_bm(int32_t dtype, int d, bool dma, int64_t pairs, int rows) {
+    return ra_shared(pairs * ((rows + 127) / 128)) ? 128 / ra_wide_of(dtype, ra_dp(d, dma)) : 128;
+}
+// lines of sums by distance that a head and sample's blocks of queries leave
+static int ra_lines(const lpm_attn_geom& g, int32_t dtype, bool dma) {
+    const int bm = ra_bm(dtype, g.d, dma, (int64_t)g.m * g.heads, g.pq);
+    return (g.pq + bm - 1) / bm * RA_WAVES;
+}
 // The forward pass's blocks: rows folded over the heads that share keys where these fit two operands of 32 rows, and the keys over several blocks where they
 // are long and the blocks do not fill the card.
 struct RaForward { bool fold; int bm, splits; };
@@ -1133,22 +1143,21 @@ static RaForward ra_plan(const lpm_attn_geom& g, int32_t dtype) {
     f.fold = share > 1 && g.pq <= 32 && share * g.pq <= 64 && share * ra_lut(g.reach) <= 8192;
     const int rows = f.fold ? share * g.pq : g.pq;
     const int64_t pairs = (int64_t)g.m * (f.fold ? g.kv_heads : g.heads);
-    f.bm = ra_bm(dtype, g.d, pairs, rows);
+    f.bm = ra_bm(dtype, g.d, false, pairs, rows);
     const int64_t blocks = std::max<int64_t>(1, pairs * ((rows + f.bm - 1) / f.bm));
     f.splits = blocks >= 512 ? 1 : (int)std::min<int64_t>({std::max(1, g.pk / 512), (1024 + blocks - 1) / blocks, RA_MAX_SPLITS});
     return f;
 }
-struct AttnLayout { size_t part_ml, fwd_all, diag, shares, bwd_all; int lines; };
+struct AttnLayout { size_t part_ml, fwd_all, diag, shares, bwd_all; };
 static AttnLayout ra_layout(const lpm_attn_geom& g, int32_t dtype) {
     AttnLayout o;
     const RaForward f = ra_plan(g, dtype);
     const size_t rows = (size_t)g.m * g.heads * g.pq, nd = ra_distances(g.reach);
-    const int bm = ra_bm(dtype, g.d, (int64_t)g.m * g.heads, g.pq);
-    o.lines = (g.pq + bm - 1) / bm * RA_WAVES;
+    const size_t lines = std::max(ra_lines(g, dtype, false), ra_lines(g, dtype, true));      // (what a call's pointers decide is not known here)
     o.part_ml = f.splits > 1 ? ra_up((size_t)f.splits * rows * g.d * 4) : 0;
     o.fwd_all = f.splits > 1 ? o.part_ml + ra_up((size_t)f.splits * rows * 8) : 0;
     o.diag = ra_up(rows * 4);
-    o.shares = o.diag + (g.n_buckets ? ra_up((size_t)g.m * g.heads * o.lines * nd * 4) : 0);
+    o.shares = o.diag + (g.n_buckets ? ra_up((size_t)g.m * g.heads * lines * nd * 4) : 0);
     o.bwd_all = o.shares + (g.n_buckets ? ra_up((size_t)RA_SHARES * g.heads * nd * 4) : 0);
     return o;
 }
@@ -1311,13 +1320,13 @@ extern "C" int32_t lpm_attn_backward(const lpm_attn_geom* geom, int32_t dtype, c
     a.diag = dtable ? (float*)((char*)ws + o.diag) : nullptr;
     hipStream_t st = (hipStream_t)stream;
     const bool dma_k = ra_dma(dtype, g.d, k, g.ldk, v, g.ldv), dma_q = ra_dma(dtype, g.d, q, g.ldq, dy, g.ldy);
-    if (queries) LPM_HIP(LPM_RA(ra_backward_q, dtype, ra_bm(dtype, g.d, (int64_t)g.m * g.heads, g.pq) < 128, dma_k));
-    if (keys) LPM_HIP(LPM_RA(ra_backward_kv, dtype, ra_bm(dtype, g.d, (int64_t)g.m * g.kv_heads, g.pk) < 128, dma_q));
+    if (queries) LPM_HIP(LPM_RA(ra_backward_q, dtype, ra_bm(dtype, g.d, dma_k, (int64_t)g.m * g.heads, g.pq) < 128, dma_k));
+    if (keys) LPM_HIP(LPM_RA(ra_backward_kv, dtype, ra_bm(dtype, g.d, dma_q, (int64_t)g.m * g.kv_heads, g.pk) < 128, dma_q));
     if (dtable) {
         const int nd = 2 * g.reach + 1;
         float* shares = (float*)((char*)ws + o.shares);
         hipLaunchKernelGGL(relattn_diagonals, dim3((unsigned)((nd + 63) / 64), (unsigned)g.heads, RA_SHARES), dim3(RA_THREADS), 0, st, (const float*)a.diag, g.m,
-                           g.heads, o.lines, nd, shares);
+                           g.heads, ra_lines(g, dtype, dma_k), nd, shares);
         hipLaunchKernelGGL(relattn_buckets, dim3((unsigned)g.heads), dim3(RA_THREADS), (size_t)nd * 8, st, (const float*)shares, map, g.heads, g.n_buckets, nd, dtable,
                            accumulate);
         LPM_HIP(hipGetLastError());
