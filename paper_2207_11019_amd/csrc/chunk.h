@@ -2,6 +2,7 @@
 #pragma once
 #include "elem.h"
 #include <cstring>
+#include <type_traits>
 
 namespace lpm {
 
@@ -18,16 +19,69 @@ __device__ __forceinline__ void st_chunk(bf16_t* p, const float (&v)[8]) {
     const uint32_t w[4] = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
     __builtin_memcpy(p, w, 16);
 }
-// ... the first n of them, 0 beyond (n may be negative or more than eight)
-template <typename T> __device__ __forceinline__ void ld_chunk(const T* p, int n, float (&v)[8]) {
-    if (n >= 8) { ld_chunk(p, v); return; }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < n ? ld(p, e) : 0.f;
-}
+// ... the first n of them (n may be negative or more than eight)
 template <typename T> __device__ __forceinline__ void st_chunk(T* p, int n, const float (&v)[8]) {
     if (n >= 8) { st_chunk(p, v); return; }
 #pragma unroll
     for (int e = 0; e < 8; ++e) if (e < n) st(p, e, v[e]);
+}
+
+// A chunk as it lies in memory, for loads that are asked for long before they are used: what converts it waits for it.
+template <typename T> struct RawChunk { uint32_t w[2 * sizeof(T)]; };
+// Chunk c (a multiple of eight) of a row of C channels.  Where the row ends inside it, its last eight channels are loaded (shift_chunk puts them in place); of
+// chunks behind the end, the row's first.
+template <typename T> __device__ __forceinline__ RawChunk<T> ld_raw(const T* row, int c, int C) {
+    RawChunk<T> r;
+    if (C >= 8) {
+        __builtin_memcpy(r.w, row + (c >= C ? 0 : c + 8 > C ? C - 8 : c), 8 * sizeof(T));
+    } else {
+        T e[8] = {};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) if (k < C) e[k] = row[k];
+        __builtin_memcpy(r.w, e, sizeof r.w);
+    }
+    return r;
+}
+__device__ __forceinline__ void raw_values(const RawChunk<float>& r, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(r.w[e]);
+}
+__device__ __forceinline__ void raw_values(const RawChunk<bf16_t>& r, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(r.w[e] << 16); v[2 * e + 1] = __uint_as_float(r.w[e] & 0xffff0000u); }
+}
+// v[e] = v[e + s], zeros behind
+__device__ __forceinline__ void shift_chunk(float (&v)[8], int s) {
+#pragma unroll
+    for (int b = 1; b < 8; b <<= 1)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = s & b ? (e + b < 8 ? v[e + b] : 0.f) : v[e];
+}
+// the values of chunk c as ld_raw brought it; zeros behind the row's end, and everywhere where it is not `there`
+template <typename T> __device__ __forceinline__ void chunk_values(const RawChunk<T>& r, int c, int C, bool there, float (&v)[8]) {
+    raw_values(r, v);
+    if (C % 8 && C > 8) shift_chunk(v, c < C && c + 8 > C ? c + 8 - C : 0);
+    if (!there || c >= C)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0.f;
+}
+
+// Sum of a value over groups of G lanes (4 to 64), the nearest by exchanges inside the vector unit
+template <int G> __device__ __forceinline__ float group_sum(float v) {
+#ifdef __HIP__
+    auto dpp = [](float x, auto ctrl) __attribute__((always_inline)) {
+        return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(x), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    v += dpp(v, std::integral_constant<int, 0xb1>());                    // lane ^ 1
+    v += dpp(v, std::integral_constant<int, 0x4e>());                    // lane ^ 2
+    if (G >= 8) v += dpp(v, std::integral_constant<int, 0x141>());       // the other four of eight
+    if (G >= 16) v += dpp(v, std::integral_constant<int, 0x140>());      // the other eight of sixteen
+    if (G >= 32) v += __shfl_xor(v, 16, 64);
+    if (G >= 64) v += __shfl_xor(v, 32, 64);
+#else
+    for (int o = 1; o < G; o <<= 1) v += __shfl_xor(v, o, 64);
+#endif
+    return v;
 }
 
 // ---- checkpoints in 8 bits ----

@@ -26,21 +26,23 @@ __global__ void __launch_bounds__(CKPT_THREADS) ckpt_pack_kernel(int64_t rows, i
     const int64_t first = (int64_t)blockIdx.x * (CKPT_ITEMS * CKPT_THREADS);
     CkptPlace b{first / per, 0, per, div};
     b.part0 = (int)(first - b.row0 * per);
-    float v[CKPT_ITEMS][8];
+    RawChunk<T> raw[CKPT_ITEMS];
     int64_t row[CKPT_ITEMS];
     int c[CKPT_ITEMS], n[CKPT_ITEMS];
 #pragma unroll
     for (int i = 0; i < CKPT_ITEMS; ++i) {
         ckpt_locate(b, i * CKPT_THREADS + (int)threadIdx.x, row[i], c[i]);
         n[i] = row[i] < rows ? C - c[i] : 0;
-        ld_chunk(n[i] > 0 ? x + row[i] * C + c[i] : x, n[i], v[i]);
+        raw[i] = ld_raw(x + (row[i] < rows ? row[i] : 0) * C, c[i], C);
     }
 #pragma unroll
     for (int i = 0; i < CKPT_ITEMS; ++i) {
-        uint32_t top = chunk_top(v[i]);
+        float v[8];
+        chunk_values(raw[i], c[i], C, row[i] < rows, v);
+        uint32_t top = chunk_top(v);
         for (int o = 1; o < 4; o <<= 1) { const uint32_t a = (uint32_t)__shfl_xor((int)top, o, 64); top = a > top ? a : top; }
         const uint32_t byte = ckpt_byte(top);
-        if (n[i] > 0) st_bytes8(q + row[i] * C + c[i], n[i], ckpt_quantise(v[i], byte));
+        if (n[i] > 0) st_bytes8(q + row[i] * C + c[i], n[i], ckpt_quantise(v, byte));
         if (n[i] > 0 && c[i] % CKPT_BLOCK == 0) ex[row[i] * ckpt_blocks(C) + c[i] / CKPT_BLOCK] = (uint8_t)byte;
     }
 }

@@ -14,16 +14,14 @@ using namespace lpm;
 
 namespace lpm {
 
-constexpr int NORM_THREADS = 256;
-constexpr int NORM_MAX_C = 16384;          // what a block of 256 threads keeps in registers, 64 channels a thread
+constexpr int norm_threads(int g) { return g < 256 ? 256 : g; }      // of a block, with G threads a row
+constexpr int NORM_MAX_C = 16384;          // what a block of 512 threads keeps in registers, 32 channels a thread
 
 // Sums of N values over the G threads of a row; `red` holds N values per wavefront where the row is the block's.
 template <int G, int N>
 __device__ __forceinline__ void norm_sum(float (&a)[N], float* red) {
 #pragma unroll
-    for (int o = 1; o < (G < 64 ? G : 64); o <<= 1)
-#pragma unroll
-        for (int i = 0; i < N; ++i) a[i] += __shfl_xor(a[i], o, 64);
+    for (int i = 0; i < N; ++i) a[i] = group_sum<(G < 64 ? G : 64)>(a[i]);
     if (G > 64) {
         const int wave = threadIdx.x >> 6;
         __syncthreads();                   // (the values of the sum before have been read)
@@ -31,28 +29,43 @@ __device__ __forceinline__ void norm_sum(float (&a)[N], float* red) {
         for (int i = 0; i < N; ++i) if ((threadIdx.x & 63) == 0) red[N * wave + i] = a[i];
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < N; ++i) a[i] = (red[i] + red[N + i]) + (red[2 * N + i] + red[3 * N + i]);
+        for (int i = 0; i < N; ++i) {
+            a[i] = red[i];
+#pragma unroll
+            for (int w = 1; w < G / 64; ++w) a[i] += red[N * w + i];
+        }
     }
 }
 
 // CH chunks of eight channels a thread: chunk k of thread t of the row's G is channel 8 (t + G k)
 template <typename T, int G, int CH>
-__global__ void __launch_bounds__(NORM_THREADS) norm_fwd_kernel(int64_t rows, int C, const T* x, const float* __restrict__ gamma, const float* __restrict__ beta,
+__global__ void __launch_bounds__(norm_threads(G)) norm_fwd_kernel(int64_t rows, int C, const T* x, const float* __restrict__ gamma, const float* __restrict__ beta,
                                                                 float eps, T* y, float* __restrict__ stats, uint8_t* __restrict__ q, uint8_t* __restrict__ ex) {
-    constexpr int RB = NORM_THREADS / G;
-    __shared__ float red[8];
+    constexpr int RB = norm_threads(G) / G;
+    __shared__ float red[16];
     const int t = threadIdx.x % G, sub = threadIdx.x / G;
+    float w[CH][8], b[CH][8];
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+        const int c = 8 * (t + G * k);
+        if (gamma) chunk_values(ld_raw(gamma, c, C), c, C, true, w[k]);
+        if (beta) chunk_values(ld_raw(beta, c, C), c, C, true, b[k]);
+    }
+    RawChunk<T> raw[CH];                   // the next row's
+    auto load = [&](int64_t row) __attribute__((always_inline)) {
+        const T* xr = x + (row < rows ? row : 0) * C;
+#pragma unroll
+        for (int k = 0; k < CH; ++k) raw[k] = ld_raw(xr, 8 * (t + G * k), C);
+    };
+    load((int64_t)blockIdx.x * RB + sub);
     for (int64_t r0 = (int64_t)blockIdx.x * RB; r0 < rows; r0 += (int64_t)gridDim.x * RB) {
         const int64_t row = r0 + sub;
         const bool there = row < rows;
-        const T* xr = x + (there ? row : 0) * C;
         float v[CH][8];
         float s[1] = {0.f};
 #pragma unroll
-        for (int k = 0; k < CH; ++k) {
-            const int c = 8 * (t + G * k), n = there ? C - c : 0;
-            ld_chunk(n > 0 ? xr + c : xr, n, v[k]);
-        }
+        for (int k = 0; k < CH; ++k) chunk_values(raw[k], 8 * (t + G * k), C, there, v[k]);
+        if (r0 + (int64_t)gridDim.x * RB < rows) load(row + (int64_t)gridDim.x * RB);
         if (q) {
 #pragma unroll
             for (int k = 0; k < CH; ++k) {
@@ -90,14 +103,11 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_fwd_kernel(int64_t rows, in
         for (int k = 0; k < CH; ++k) {
             const int c = 8 * (t + G * k), n = there ? C - c : 0;
             if (n <= 0) continue;
-            float w[8], b[8];
-            if (gamma) ld_chunk(gamma + c, n, w);
-            if (beta) ld_chunk(beta + c, n, b);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 float h = (v[k][e] - mu) * rs;
-                if (gamma) h *= w[e];
-                v[k][e] = beta ? h + b[e] : h;
+                if (gamma) h *= w[k][e];
+                v[k][e] = beta ? h + b[k][e] : h;
             }
             st_chunk(y + row * C + c, n, v[k]);
         }
@@ -105,48 +115,69 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_fwd_kernel(int64_t rows, in
 }
 
 // part (NULL: no weight gradients): [gridDim.x][2][C], the block's sums of dy h and of dy
-template <typename T, int G, int CH>
-__global__ void __launch_bounds__(NORM_THREADS) norm_bwd_kernel(int64_t rows, int C, const T* x, const uint8_t* __restrict__ q, const uint8_t* __restrict__ ex,
+template <typename T, int G, int CH, bool KEPT>
+__global__ void __launch_bounds__(norm_threads(G)) norm_bwd_kernel(int64_t rows, int C, const T* x, const uint8_t* __restrict__ q, const uint8_t* __restrict__ ex,
                                                                 const float* __restrict__ stats, const T* dy, const float* __restrict__ gamma, T* dx,
                                                                 int accumulate, float* __restrict__ part) {
-    constexpr int RB = NORM_THREADS / G;
-    __shared__ float red[8];
+    constexpr int RB = norm_threads(G) / G;
+    __shared__ float red[16];
     const int t = threadIdx.x % G, sub = threadIdx.x / G;
     const float inv = 1.f / (float)C;
-    float dg[CH][8], db[CH][8];
+    float dg[CH][8], db[CH][8], w[CH][8];
 #pragma unroll
-    for (int k = 0; k < CH; ++k)
+    for (int k = 0; k < CH; ++k) {
+        const int c = 8 * (t + G * k);
+        if (gamma) chunk_values(ld_raw(gamma, c, C), c, C, true, w[k]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) dg[k][e] = db[k][e] = 0.f;
+    }
+    // the next row's
+    RawChunk<T> raw_g[CH], raw_x[KEPT ? 1 : CH];
+    uint2 raw_q[KEPT ? CH : 1];
+    uint32_t raw_e[KEPT ? CH : 1];
+    float raw_mu, raw_rs;
+    auto load = [&](int64_t row) __attribute__((always_inline)) {
+        const int64_t from = row < rows ? row : 0;
+        raw_mu = stats[2 * from];
+        raw_rs = stats[2 * from + 1];
+#pragma unroll
+        for (int k = 0; k < CH; ++k) {
+            const int c = 8 * (t + G * k);
+            raw_g[k] = ld_raw(dy + from * C, c, C);
+            if constexpr (KEPT) {
+                raw_q[k] = ld_bytes8(q + from * C + (c < C ? c : 0), c < C ? C - c : 0);
+                raw_e[k] = ex[from * ckpt_blocks(C) + (c < C ? c / CKPT_BLOCK : 0)];
+            } else {
+                raw_x[k] = ld_raw(x + from * C, c, C);
+            }
+        }
+    };
+    constexpr bool AHEAD = G < 512;        // (of the longest rows there is no room for two)
+    if (AHEAD) load((int64_t)blockIdx.x * RB + sub);
     for (int64_t r0 = (int64_t)blockIdx.x * RB; r0 < rows; r0 += (int64_t)gridDim.x * RB) {
         const int64_t row = r0 + sub;
         const bool there = row < rows;
         const int64_t base = (there ? row : 0) * C;
-        const float mu = there ? stats[2 * row] : 0.f, rs = there ? stats[2 * row + 1] : 0.f;
+        if (!AHEAD) load(row);
+        const float mu = raw_mu, rs = raw_rs;
         float h[CH][8], g[CH][8];
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
-            const int c = 8 * (t + G * k), n = there ? C - c : 0;
-            const int64_t o = n > 0 ? base + c : 0;
-            ld_chunk(dy + o, n, g[k]);
-            if (q) {
-                const uint32_t byte = n > 0 ? ex[row * ckpt_blocks(C) + c / CKPT_BLOCK] : 1u;
-                ckpt_values(ld_bytes8(q + o, n), byte, h[k]);
-            } else {
-                ld_chunk(x + o, n, h[k]);
-            }
+            const int c = 8 * (t + G * k);
+            chunk_values(raw_g[k], c, C, there, g[k]);
+            if constexpr (KEPT) ckpt_values(raw_q[k], raw_e[k], h[k]);
+            else chunk_values(raw_x[k], c, C, there, h[k]);
         }
+        if (AHEAD && r0 + (int64_t)gridDim.x * RB < rows) load(row + (int64_t)gridDim.x * RB);
         float sums[2] = {0.f, 0.f};             // of g and of g h
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
             const int c = 8 * (t + G * k), n = there ? C - c : 0;
-            float w[8];
-            if (gamma) ld_chunk(n > 0 ? gamma + c : gamma, n, w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 h[k][e] = e < n ? (h[k][e] - mu) * rs : 0.f;
                 if (part) { dg[k][e] = fmaf(g[k][e], h[k][e], dg[k][e]); db[k][e] += g[k][e]; }
-                if (gamma) g[k][e] *= w[e];
+                if (gamma) g[k][e] *= w[k][e];
                 sums[0] += g[k][e];
                 sums[1] = fmaf(g[k][e], h[k][e], sums[1]);
             }
@@ -162,7 +193,7 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_bwd_kernel(int64_t rows, in
             for (int e = 0; e < 8; ++e) v[e] = rs * (g[k][e] - mg - h[k][e] * mgh);
             if (accumulate) {
                 float old[8];
-                ld_chunk(dx + base + c, n, old);
+                chunk_values(ld_raw(dx + base, c, C), c, C, true, old);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] += old[e];
             }
@@ -202,20 +233,25 @@ __global__ void __launch_bounds__(NORM_THREADS) norm_bwd_kernel(int64_t rows, in
     }
 }
 
-// dst[c] (+)= the sum over blocks of part[block][c], for the 2 C columns (dgamma, then dbeta): a block has 32 columns, eight threads share one, each
-// its eighth of the blocks
+// dst[c] (+)= the sum over blocks of part[block][c], for the 2 C columns (dgamma, then dbeta): a block has 16 columns, sixteen threads share one, each its
+// sixteenth of the blocks, eight loads at a time
 __global__ void __launch_bounds__(256) norm_columns_kernel(const float* __restrict__ part, int blocks, int C, float* __restrict__ dgamma, float* __restrict__ dbeta,
                                                            int accumulate) {
-    __shared__ float sums[8][32];
-    const int lane = threadIdx.x & 31, share = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
+    __shared__ float sums[16][17];
+    const int lane = threadIdx.x & 15, share = threadIdx.x >> 4, col = blockIdx.x * 16 + lane, from = min(col, 2 * C - 1);
     float s = 0.f;
-    if (col < 2 * C)
-        for (int b = share; b < blocks; b += 8) s += part[(int64_t)b * 2 * C + col];
+    for (int b = share; b < blocks; b += 128) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = part[(int64_t)min(b + 16 * k, blocks - 1) * 2 * C + from];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += b + 16 * k < blocks ? v[k] : 0.f;
+    }
     sums[share][lane] = s;
     __syncthreads();
     if (share || col >= 2 * C) return;
 #pragma unroll
-    for (int k = 1; k < 8; ++k) s += sums[k][lane];
+    for (int k = 1; k < 16; ++k) s += sums[k][lane];
     float* dst = col < C ? dgamma : dbeta;
     if (!dst) return;
     const int c = col < C ? col : col - C;
@@ -228,11 +264,11 @@ static NormShape norm_shape(int C) {
     for (int g = 4; g <= 64; g *= 2) if (C <= 8 * g) return {g, 1};
     for (int ch = 2; ch <= 4; ch *= 2) if (C <= 512 * ch) return {64, ch};
     for (int ch = 2; ch <= 4; ch *= 2) if (C <= 2048 * ch) return {256, ch};
-    return {256, 8};
+    return {512, 4};
 }
 // blocks of the backward pass: each adds a line of 2 C floats to what the second kernel reads
 static int norm_bwd_blocks(int64_t rows, int C) {
-    const int per = NORM_THREADS / norm_shape(C).g;
+    const int per = norm_threads(norm_shape(C).g) / norm_shape(C).g;
     const int64_t b = (rows + per - 1) / per;
     return (int)(b < 512 ? b : 512);
 }
@@ -247,17 +283,17 @@ static int norm_bwd_blocks(int64_t rows, int C) {
         else if (sh__.g == 64 && sh__.ch == 2) { constexpr int G = 64, CH = 2; __VA_ARGS__; }    \
         else if (sh__.g == 64) { constexpr int G = 64, CH = 4; __VA_ARGS__; }                    \
         else if (sh__.ch == 2) { constexpr int G = 256, CH = 2; __VA_ARGS__; }                   \
-        else if (sh__.ch == 4) { constexpr int G = 256, CH = 4; __VA_ARGS__; }                   \
-        else { constexpr int G = 256, CH = 8; __VA_ARGS__; }                                     \
+        else if (sh__.g == 256) { constexpr int G = 256, CH = 4; __VA_ARGS__; }                   \
+        else { constexpr int G = 512, CH = 4; __VA_ARGS__; }                                     \
     } while (0)
 
 template <typename T>
 static hipError_t norm_fwd(int64_t rows, int C, const T* x, const float* gamma, const float* beta, float eps, T* y, float* stats, uint8_t* q, uint8_t* ex,
                            hipStream_t st) {
-    const int per = NORM_THREADS / norm_shape(C).g;
+    const int per = norm_threads(norm_shape(C).g) / norm_shape(C).g;
     const int64_t b = (rows + per - 1) / per;
-    const dim3 grid((unsigned)(b < 8192 ? b : 8192));
-    LPM_NORM_SHAPE(C, hipLaunchKernelGGL((norm_fwd_kernel<T, G, CH>), grid, dim3(NORM_THREADS), 0, st, rows, C, x, gamma, beta, eps, y, stats, q, ex));
+    const dim3 grid((unsigned)(b < 2048 ? b : 2048));
+    LPM_NORM_SHAPE(C, hipLaunchKernelGGL((norm_fwd_kernel<T, G, CH>), grid, dim3(norm_threads(G)), 0, st, rows, C, x, gamma, beta, eps, y, stats, q, ex));
     return hipGetLastError();
 }
 template <typename T>
@@ -266,9 +302,11 @@ static hipError_t norm_bwd(int64_t rows, int C, const T* x, const uint8_t* q, co
     const bool sums = dgamma || dbeta;
     const int blocks = norm_bwd_blocks(rows, C);
     if (rows > 0)
-        LPM_NORM_SHAPE(C, hipLaunchKernelGGL((norm_bwd_kernel<T, G, CH>), dim3((unsigned)blocks), dim3(NORM_THREADS), 0, st, rows, C, x, q, ex, stats, dy, gamma,
-                                             dx, dx_acc, sums ? ws : nullptr));
-    if (sums) hipLaunchKernelGGL(norm_columns_kernel, dim3((unsigned)((2 * C + 31) / 32)), dim3(256), 0, st, (const float*)ws, blocks, C, dgamma, dbeta, accumulate);
+        LPM_NORM_SHAPE(C, if (q) hipLaunchKernelGGL((norm_bwd_kernel<T, G, CH, true>), dim3((unsigned)blocks), dim3(norm_threads(G)), 0, st, rows, C, x, q, ex, stats,
+                                                    dy, gamma, dx, dx_acc, sums ? ws : nullptr);
+                          else hipLaunchKernelGGL((norm_bwd_kernel<T, G, CH, false>), dim3((unsigned)blocks), dim3(norm_threads(G)), 0, st, rows, C, x, q, ex, stats,
+                                                  dy, gamma, dx, dx_acc, sums ? ws : nullptr));
+    if (sums) hipLaunchKernelGGL(norm_columns_kernel, dim3((unsigned)((2 * C + 15) / 16)), dim3(256), 0, st, (const float*)ws, blocks, C, dgamma, dbeta, accumulate);
     return hipGetLastError();
 }
 
