@@ -281,23 +281,56 @@ def _elem(dtype):
 _NAMES = {F32: "torch.float32", BF16: "torch.bfloat16"}
 
 
-def _takes(name, t, nbytes, kind=None):
-    """_holds, and for the operators whose operands are tensors of one element type: that type (or bytes), dense, on the current GPU."""
-    if t is None or isinstance(t, int):
-        return
-    if kind is not None and str(t.dtype) not in (kind, "torch.uint8"):
-        raise ValueError("%s is a tensor of %s, the call takes %s" % (name, t.dtype, kind))
-    if not t.is_contiguous():
-        raise ValueError("%s is not dense" % name)
-    _on_this_gpu(name, t)
-    _holds(name, t, nbytes)
+_kinds = {}
 
 
-def _on_this_gpu(name, t):
-    if t.is_cuda:
-        import torch
-        if t.device.index != torch.cuda.current_device():
-            raise ValueError("%s is on %s, the current device is %d" % (name, t.device, torch.cuda.current_device()))
+class _Operands:
+    """The tensors of one call to an operator: of the element type that it takes (or bytes) and of the current GPU."""
+
+    def __init__(self):
+        self.gpu = None
+
+    def of(self, name, t, kind):
+        have = _kinds.get(t.dtype) or _kinds.setdefault(t.dtype, str(t.dtype))
+        if kind is not None and have != kind and have != "torch.uint8":
+            raise ValueError("%s is a tensor of %s, the call takes %s" % (name, have, kind))
+        at = t.get_device()
+        if at != self.gpu and (at >= 0 or self.gpu is not None or _gpu_works()):
+            import torch
+            if at < 0:
+                raise ValueError("%s is in host memory" % name)
+            if self.gpu is None:
+                self.gpu = torch.cuda.current_device()
+            if at != self.gpu:
+                raise ValueError("%s is on GPU %d, the current device is %d" % (name, at, self.gpu))
+
+    def takes(self, name, t, nbytes, kind=None):
+        """dense, with room for nbytes"""
+        if t is None or isinstance(t, int):
+            return
+        self.of(name, t, kind)
+        if not t.is_contiguous():
+            raise ValueError("%s is not dense" % name)
+        _holds(name, t, nbytes)
+
+    def spaced(self, name, t, dtype, positions, ld, width):
+        """The operand's positions, `ld` elements apart from its first element on, lie inside the tensor's memory: it may be a part of a packed tensor."""
+        if t is None or isinstance(t, int) or positions == 0:
+            return
+        self.of(name, t, None)
+        if _kinds[t.dtype] != _NAMES[dtype]:
+            raise ValueError("%s is a tensor of %s, the call takes %s" % (name, t.dtype, _NAMES[dtype]))
+        if t.dim() > 0 and t.stride(-1) != 1 and t.shape[-1] > 1:
+            raise ValueError("%s: the channels of a position do not lie side by side" % name)
+        have = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+        need = (positions - 1) * (ld or width) + width
+        if have < need:
+            raise ValueError("%s reaches over %d elements, the geometry needs %d" % (name, have, need))
+
+
+def _gpu_works():
+    import torch
+    return torch.cuda.device_count() > 0
 
 
 def lpm_ckpt8_bytes(rows, channels):
@@ -310,14 +343,16 @@ def lpm_ckpt8_bytes(rows, channels):
 def lpm_ckpt8_pack(rows, channels, dtype, x, ckpt, stream=None):
     """ckpt = the 8-bit checkpoint of x."""
     kept = lpm_ckpt8_bytes(rows, channels)
-    _takes("x", x, rows * channels * _elem(dtype), _NAMES.get(dtype)), _takes("ckpt", ckpt, kept)
+    on = _Operands()
+    on.takes("x", x, rows * channels * _elem(dtype), _NAMES.get(dtype)), on.takes("ckpt", ckpt, kept)
     _check(lib.lpm_ckpt8_pack(rows, channels, dtype, _ptr(x), _ptr(ckpt), _stream(stream)))
 
 
 def lpm_ckpt8_unpack(rows, channels, dtype, ckpt, x, stream=None):
     """x = the values that ckpt stands for."""
     kept = lpm_ckpt8_bytes(rows, channels)
-    _takes("x", x, rows * channels * _elem(dtype), _NAMES.get(dtype)), _takes("ckpt", ckpt, kept)
+    on = _Operands()
+    on.takes("x", x, rows * channels * _elem(dtype), _NAMES.get(dtype)), on.takes("ckpt", ckpt, kept)
     _check(lib.lpm_ckpt8_unpack(rows, channels, dtype, _ptr(ckpt), _ptr(x), _stream(stream)))
 
 
@@ -332,8 +367,9 @@ def lpm_conv_wgrad_ckpt8(g, dtype, ckpt, dz, dw, accumulate=False, ws=None, stre
     gg = _geom(g)
     need = lpm_conv_wgrad_ckpt8_ws_bytes(gg, dtype)
     _, yb, _, db = _conv_sizes(gg, dtype)
-    _takes("ckpt", ckpt, lpm_ckpt8_bytes(gg.m * max(gg.d, 1) * gg.h * gg.w, gg.cin)), _takes("dz", dz, yb, _NAMES.get(dtype))
-    _takes("dw", dw, db, _NAMES[F32]), _takes("ws", ws, need)
+    on = _Operands()
+    on.takes("ckpt", ckpt, lpm_ckpt8_bytes(gg.m * max(gg.d, 1) * gg.h * gg.w, gg.cin)), on.takes("dz", dz, yb, _NAMES.get(dtype))
+    on.takes("dw", dw, db, _NAMES[F32]), on.takes("ws", ws, need)
     _check(lib.lpm_conv_wgrad_ckpt8(C.byref(gg), dtype, _ptr(ckpt), _ptr(dz), _ptr(dw), int(accumulate), _ptr(ws), _stream(stream)))
 
 
@@ -344,15 +380,15 @@ def lpm_norm_ws_bytes(rows, channels, dtype):
     return n.value
 
 
-def _norm_holds(rows, channels, dtype, full, line, stats, ckpt):
-    lpm_norm_ws_bytes(rows, channels, dtype)      # (refuses a bad shape before sizes are worked out from it)
+def _norm_holds(rows, channels, dtype, full, line, stats, ckpt, ws=None):
+    need, on = lpm_norm_ws_bytes(rows, channels, dtype), _Operands()      # (refuses a bad shape before sizes are worked out from it)
     for name, t in full.items():
-        _takes(name, t, rows * channels * _elem(dtype), _NAMES[dtype])
+        on.takes(name, t, rows * channels * _elem(dtype), _NAMES[dtype])
     for name, t in line.items():
-        _takes(name, t, channels * 4, _NAMES[F32])
-    _takes("stats", stats, rows * 8, _NAMES[F32])
+        on.takes(name, t, channels * 4, _NAMES[F32])
+    on.takes("stats", stats, rows * 8, _NAMES[F32]), on.takes("ws", ws, need)
     if ckpt is not None:
-        _takes("ckpt", ckpt, lpm_ckpt8_bytes(rows, channels))
+        on.takes("ckpt", ckpt, lpm_ckpt8_bytes(rows, channels))
 
 
 def lpm_norm_forward(rows, channels, dtype, x, gamma, beta, eps, y, stats=None, ckpt=None, stream=None):
@@ -364,8 +400,7 @@ def lpm_norm_forward(rows, channels, dtype, x, gamma, beta, eps, y, stats=None, 
 def lpm_norm_backward(rows, channels, dtype, x, ckpt, stats, dy, gamma, dx, dgamma=None, dbeta=None, dx_accumulate=False, accumulate=False, ws=None,
                       stream=None):
     """Gradients of lpm_norm_forward from the input x or its checkpoint (the other one None)."""
-    _norm_holds(rows, channels, dtype, dict(x=x, dy=dy, dx=dx), dict(gamma=gamma, dgamma=dgamma, dbeta=dbeta), stats, ckpt)
-    _takes("ws", ws, lpm_norm_ws_bytes(rows, channels, dtype))
+    _norm_holds(rows, channels, dtype, dict(x=x, dy=dy, dx=dx), dict(gamma=gamma, dgamma=dgamma, dbeta=dbeta), stats, ckpt, ws)
     _check(lib.lpm_norm_backward(rows, channels, dtype, _ptr(x), _ptr(ckpt), _ptr(stats), _ptr(dy), _ptr(gamma), _ptr(dx), int(dx_accumulate),
                                  _ptr(dgamma), _ptr(dbeta), int(accumulate), _ptr(ws), _stream(stream)))
 
@@ -388,41 +423,26 @@ def lpm_attn_stats_bytes(g, dtype):
     return n.value
 
 
-def _spaced(name, t, dtype, positions, ld, width):
-    """The operand's positions, `ld` elements apart from its first element on, lie inside the tensor's memory: it may be a part of a packed tensor."""
-    if t is None or isinstance(t, int) or positions == 0:
-        return
-    if str(t.dtype) != _NAMES[dtype]:
-        raise ValueError("%s is a tensor of %s, the call takes %s" % (name, t.dtype, _NAMES[dtype]))
-    if t.dim() > 0 and t.stride(-1) != 1 and t.shape[-1] > 1:
-        raise ValueError("%s: the channels of a position do not lie side by side" % name)
-    _on_this_gpu(name, t)
-    have = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
-    need = (positions - 1) * (ld or width) + width
-    if have < need:
-        raise ValueError("%s reaches over %d elements, the geometry needs %d" % (name, have, need))
-
-
-def _attn_holds(g, dtype, spaced, samples, bias, stats):
-    lpm_attn_ws_bytes(g, dtype)                   # (refuses a bad shape before sizes are worked out from it)
+def _attn_holds(g, dtype, spaced, samples, bias, stats, ws, backward):
+    need, on = lpm_attn_ws_bytes(g, dtype)[backward], _Operands()         # (refuses a bad shape before sizes are worked out from it)
     wq, wk = g.heads * g.d, g.kv_heads * g.d
     for name, t in spaced.items():
         kv = name.lstrip("d") in ("k", "v")
-        _spaced(name, t, dtype, g.m * (g.pk if kv else g.pq), getattr(g, "ld" + name.lstrip("d")), wk if kv else wq)
+        on.spaced(name, t, dtype, g.m * (g.pk if kv else g.pq), getattr(g, "ld" + name.lstrip("d")), wk if kv else wq)
     for name, t in samples.items():
-        _takes(name, t, 4 * g.m, "torch.int32")
-    _takes("map", bias[0], 4 * (2 * g.reach + 1), "torch.int32")
+        on.takes(name, t, 4 * g.m, "torch.int32")
+    on.takes("map", bias[0], 4 * (2 * g.reach + 1), "torch.int32")
     for t in bias[1:]:
-        _takes("table", t, 4 * g.heads * g.n_buckets, _NAMES[F32])
+        on.takes("table", t, 4 * g.heads * g.n_buckets, _NAMES[F32])
+    on.takes("ws", ws, need)
     if stats is not None:
-        _takes("stats", stats, lpm_attn_stats_bytes(g, dtype))
+        on.takes("stats", stats, lpm_attn_stats_bytes(g, dtype))
 
 
 def lpm_attn_forward(g, dtype, q, k, v, key_len, q_start, map, table, y, stats=None, ws=None, stream=None):
     """Attention with the bias table[h][map[distance]]; g: an lpm_attn_geom or its fields as a dict."""
     gg = _attn_geom(g)
-    _attn_holds(gg, dtype, dict(q=q, k=k, v=v, y=y), dict(key_len=key_len, q_start=q_start), (map, table), stats)
-    _takes("ws", ws, lpm_attn_ws_bytes(gg, dtype)[0])
+    _attn_holds(gg, dtype, dict(q=q, k=k, v=v, y=y), dict(key_len=key_len, q_start=q_start), (map, table), stats, ws, 0)
     _check(lib.lpm_attn_forward(C.byref(gg), dtype, _ptr(q), _ptr(k), _ptr(v), _ptr(key_len), _ptr(q_start), _ptr(map), _ptr(table), _ptr(y), _ptr(stats),
                                 _ptr(ws), _stream(stream)))
 
@@ -430,8 +450,7 @@ def lpm_attn_forward(g, dtype, q, k, v, key_len, q_start, map, table, y, stats=N
 def lpm_attn_backward(g, dtype, q, k, v, y, stats, dy, key_len, q_start, map, table, dq, dk, dv, dtable=None, accumulate=False, ws=None, stream=None):
     """Gradients of lpm_attn_forward; accumulate concerns dtable."""
     gg = _attn_geom(g)
-    _attn_holds(gg, dtype, dict(q=q, k=k, v=v, y=y, dy=dy, dq=dq, dk=dk, dv=dv), dict(key_len=key_len, q_start=q_start), (map, table, dtable), stats)
-    _takes("ws", ws, lpm_attn_ws_bytes(gg, dtype)[1])
+    _attn_holds(gg, dtype, dict(q=q, k=k, v=v, y=y, dy=dy, dq=dq, dk=dk, dv=dv), dict(key_len=key_len, q_start=q_start), (map, table, dtable), stats, ws, 1)
     _check(lib.lpm_attn_backward(C.byref(gg), dtype, _ptr(q), _ptr(k), _ptr(v), _ptr(y), _ptr(stats), _ptr(dy), _ptr(key_len), _ptr(q_start), _ptr(map),
                                  _ptr(table), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dtable), int(accumulate), _ptr(ws), _stream(stream)))
 

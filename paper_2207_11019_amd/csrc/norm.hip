@@ -117,17 +117,18 @@ __global__ void __launch_bounds__(norm_threads(G)) norm_fwd_kernel(int64_t rows,
 // part (NULL: no weight gradients): [gridDim.x][2][C], the block's sums of dy h and of dy
 template <typename T, int G, int CH, bool KEPT>
 __global__ void __launch_bounds__(norm_threads(G)) norm_bwd_kernel(int64_t rows, int C, const T* x, const uint8_t* __restrict__ q, const uint8_t* __restrict__ ex,
-                                                                const float* __restrict__ stats, const T* dy, const float* __restrict__ gamma, T* dx,
+                                                                const float* __restrict__ stats, const T* dy, const float* gamma, T* dx,
                                                                 int accumulate, float* __restrict__ part) {
     constexpr int RB = norm_threads(G) / G;
     __shared__ float red[16];
     const int t = threadIdx.x % G, sub = threadIdx.x / G;
     const float inv = 1.f / (float)C;
+    constexpr bool AHEAD = G < 512;        // (of the longest rows there is no room for two, nor for the weights)
     float dg[CH][8], db[CH][8], w[CH][8];
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
         const int c = 8 * (t + G * k);
-        if (gamma) chunk_values(ld_raw(gamma, c, C), c, C, true, w[k]);
+        if (AHEAD && gamma) chunk_values(ld_raw(gamma, c, C), c, C, true, w[k]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) dg[k][e] = db[k][e] = 0.f;
     }
@@ -152,7 +153,6 @@ __global__ void __launch_bounds__(norm_threads(G)) norm_bwd_kernel(int64_t rows,
             }
         }
     };
-    constexpr bool AHEAD = G < 512;        // (of the longest rows there is no room for two)
     if (AHEAD) load((int64_t)blockIdx.x * RB + sub);
     for (int64_t r0 = (int64_t)blockIdx.x * RB; r0 < rows; r0 += (int64_t)gridDim.x * RB) {
         const int64_t row = r0 + sub;
@@ -173,6 +173,7 @@ __global__ void __launch_bounds__(norm_threads(G)) norm_bwd_kernel(int64_t rows,
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
             const int c = 8 * (t + G * k), n = there ? C - c : 0;
+            if (!AHEAD && gamma) chunk_values(ld_raw(gamma, c, C), c, C, true, w[k]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 h[k][e] = e < n ? (h[k][e] - mu) * rs : 0.f;

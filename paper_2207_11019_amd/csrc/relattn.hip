@@ -48,7 +48,7 @@ struct AttnArgs {
 // WK wavefronts share a block's 128 / WK rows, each with its 32 rows of every tile of the other side.  DMA: tiles go straight from memory to LDS (channels in
 // whole 16-byte chunks, rows on whole dwords); else by way of registers, where a row's last chunk is put in order.
 template <typename T, int DP, int WK_, bool DMA_, int OCC, bool SMALL = false> struct Ra {
-    static constexpr int WK = WK_;
+    static constexpr int WK = WK_, BLOCKS = OCC;              // wavefronts that share rows, blocks of a CU
     static constexpr bool DMA = DMA_;
     static constexpr int EPC = Mm<T>::EPC, CHUNKS = DP / EPC, KS = DP / (2 * EPC), ES = (int)sizeof(T);
     static constexpr int BM = 128 / WK;
@@ -66,7 +66,7 @@ template <typename T, int DP, int WK_, bool DMA_, int OCC, bool SMALL = false> s
     static constexpr int AREAS = ES == 2 ? 2 * STAGE : LDS, LDS_Q = AREAS + DIAGONALS > LDS ? AREAS + DIAGONALS : LDS;
     static constexpr int PER = BN * CHUNKS / RA_THREADS;      // chunks of a tile a thread brings
     static constexpr int DT = DP / 32;                        // 32-channel pieces of a head
-    static constexpr int AHEAD = DMA ? 6 : 4;                 // operands of a product on their way (8192 keys, dk and dv, 6 against 4: 847 -> 819 us)
+    static constexpr int AHEAD = DMA ? 6 : 2;                 // operands of a product on their way (8192 keys, dk and dv, 6 against 4: 847 -> 819 us)
     static constexpr int NU = 16 / EPC;                       // operands of a column of 32 probabilities
     // Chunk c of a row lies at position c ^ place(row).  A row-wise read takes one chunk of eight rows at a time, a column-wise one 64 bytes of four rows: of
     // the 256 bytes that the banks hold side by side, four consecutive rows have a quarter each, and eight rows a position each.
@@ -79,8 +79,8 @@ template <typename T, int DP, int WK_, bool DMA_, int OCC, bool SMALL = false> s
 // of 128 channels, 535 -> RA_FWD_US us.)
 template <typename T, int DP> constexpr int RA_OCC_Q = sizeof(T) == 2 || DP <= 32 ? 2 : 1;
 template <typename T, int DP> constexpr int RA_OCC_KV = DP <= 32 || (sizeof(T) == 2 && DP <= 64) ? 2 : 1;
-template <typename T, int DP, int WK, bool DMA> using RaFwd = Ra<T, DP, WK, DMA, 2, (DP > 64)>;
-template <typename T, int DP, int WK, bool DMA> using RaBwdQ = Ra<T, DP, WK, DMA, RA_OCC_Q<T, DP>, (DP > 64)>;
+template <typename T, int DP, int WK, bool DMA> using RaFwd = Ra<T, DP, WK, DMA, DMA || sizeof(T) == 2 || DP <= 64 ? 2 : 1, (DP > 64)>;
+template <typename T, int DP, int WK, bool DMA> using RaBwdQ = Ra<T, DP, WK, DMA, DMA || DP <= 64 ? RA_OCC_Q<T, DP> : 1, (DP > 64)>;
 template <typename T, int DP, int WK, bool DMA> using RaBwdKv = Ra<T, DP, WK, DMA, RA_OCC_KV<T, DP>>;
 
 // Sixteen bytes of a row of d channels from channel c on, through a buffer whose end is the last row's: rows beyond are zeros.  Where d is no whole
@@ -373,7 +373,7 @@ template <bool REVERSE> __device__ __forceinline__ RaBlock ra_block(int m, int h
 }
 
 template <typename T, int DP, int WK, bool DMA>
-__global__ void __launch_bounds__(RA_THREADS, 2) relattn_fwd(AttnArgs a) {
+__global__ void __launch_bounds__(RA_THREADS, (RaFwd<T, DP, WK, DMA>::BLOCKS)) relattn_fwd(AttnArgs a) {
     typedef RaFwd<T, DP, WK, DMA> R;
     extern __shared__ __attribute__((aligned(16))) unsigned char ra_lds[];
     int* huge = reinterpret_cast<int*>(ra_lds + R::LDS);
@@ -674,7 +674,7 @@ struct RaDiagonals {
 // the sum of a row's ds, which is 0 but for delta's error, corrects it: the sums of tiles beyond the reach afterwards, with those of p beside them,
 // while the tiles within the reach are gone through once more.  (Float: y is as exact as the rest, one walk does it all.)
 template <typename T, int DP, int WK, bool DMA>
-__global__ void __launch_bounds__(RA_THREADS, (RA_OCC_Q<T, DP>)) relattn_bwd_q(AttnArgs a) {
+__global__ void __launch_bounds__(RA_THREADS, (RaBwdQ<T, DP, WK, DMA>::BLOCKS)) relattn_bwd_q(AttnArgs a) {
     typedef RaBwdQ<T, DP, WK, DMA> R;
     extern __shared__ __attribute__((aligned(16))) unsigned char ra_lds[];
     float* areas = reinterpret_cast<float*>(ra_lds + R::AREAS);
@@ -907,7 +907,7 @@ __global__ void __launch_bounds__(RA_THREADS, (RA_OCC_Q<T, DP>)) relattn_bwd_q(A
 
 // dk and dv of a block's keys: the queries of every head that shares them, one head after the other
 template <typename T, int DP, int WK, bool DMA>
-__global__ void __launch_bounds__(RA_THREADS, (RA_OCC_KV<T, DP>)) relattn_bwd_kv(AttnArgs a) {
+__global__ void __launch_bounds__(RA_THREADS, (RaBwdKv<T, DP, WK, DMA>::BLOCKS)) relattn_bwd_kv(AttnArgs a) {
     typedef RaBwdKv<T, DP, WK, DMA> R;
     extern __shared__ __attribute__((aligned(16))) unsigned char ra_lds[];
     float* rowvs = reinterpret_cast<float*>(ra_lds + R::LDS);         // two of [4][BN]: -log2 sum less top, delta, top, -log2 sum
@@ -1213,7 +1213,7 @@ static int32_t ra_check(const lpm_attn_geom* g, int32_t dtype, lpm_attn_geom& o)
     if (o.d < 8 || o.d > 128) return fail(LPM_ESHAPE, "heads of %d channels (8 to 128)", o.d);
     if (o.n_buckets < 0 || o.n_buckets > 65536 || o.reach < 0 || o.reach > RA_MAX_REACH)
         return fail(LPM_ESHAPE, "%d buckets (0 to 65536) of distances up to %d (0 to %d)", o.n_buckets, o.reach, RA_MAX_REACH);
-    if (!(o.scale >= 0.f) || o.scale > 1e30f) return fail(LPM_EINVAL, "scale must be a number of 0 (for 1 / sqrt(d)) or more");
+    if (o.scale != 0.f && !(o.scale >= 1e-30f && o.scale <= 1e30f)) return fail(LPM_EINVAL, "scale must be 0 (for 1 / sqrt(d)) or 1e-30 to 1e30");
     const int64_t wq = (int64_t)o.heads * o.d, wk = (int64_t)o.kv_heads * o.d;
     if (wq > RA_MAX_LD) return fail(LPM_ESHAPE, "%d heads of %d channels", o.heads, o.d);
     if (!o.ldq) o.ldq = (int32_t)wq;

@@ -22,6 +22,7 @@ RUNS = [
     (0, "test_gpu_norm.py", "channels and (257 or 65 or 2056) or checkpoint and 100"),
     (1, "test_gpu_relattn.py", "not larger and not graph"),
     (0, "test_gpu_relattn.py", "test_attention and (m2_h4 or d96 or d9_)"),
+    (1, "test_gpu_operators.py", "test_block or differences or scales"),
 ]
 
 
