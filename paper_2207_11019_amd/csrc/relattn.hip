@@ -1120,31 +1120,39 @@ __global__ void __launch_bounds__(RA_THREADS) relattn_buckets(const float* __res
 }
 
 static size_t ra_up(size_t b) { return (b + 255) & ~(size_t)255; }
-// Wavefronts that share rows (and walk the other side's tiles together): where blocks of 128 rows are too few to give every CU two.
-// (As many as the tiles leave room for in LDS.)
-template <typename T, int DP> constexpr int ra_wide() { return sizeof(T) == 2 ? (DP <= 64 ? 4 : 2) : DP <= 32 ? 4 : DP <= 64 ? 2 : 1; }
+// Wavefronts that share rows (and walk the other side's tiles together), at most as many as the tiles leave room for in LDS ...
+template <typename T, int DP> constexpr int ra_most() { return sizeof(T) == 2 ? (DP <= 64 ? 4 : 2) : DP <= 32 ? 4 : DP <= 64 ? 2 : 1; }
 static int ra_dp(int d, bool dma) { return d <= 32 && dma ? 32 : d <= 64 ? 64 : d <= 96 && dma ? 96 : 128; }
-static int ra_wide_of(int32_t dtype, int dp) { return dtype == LPM_BF16 ? (dp <= 64 ? 4 : 2) : dp <= 32 ? 4 : dp <= 64 ? 2 : 1; }
-static bool ra_shared(int64_t blocks) { return blocks <= 256; }
-static int ra_bm(int32_t dtype, int d, bool dma, int64_t pairs, int rows) {
-    return ra_shared(pairs * ((rows + 127) / 128)) ? 128 / ra_wide_of(dtype, ra_dp(d, dma)) : 128;
+static int ra_most_of(int32_t dtype, int dp) { return dtype == LPM_BF16 ? (dp <= 64 ? 4 : 2) : dp <= 32 ? 4 : dp <= 64 ? 2 : 1; }
+// ... and as many as there are blocks missing: the CUs are 256, and a block of shared rows takes 0.6 (two wavefronts) or 0.46 (four) of the time of one
+// with rows for each.  (512 keys, dq: 32 float heads of 32 channels, 128 blocks of 128 rows, by wavefronts 1, 2, 4: 44, 28, 37 us; 16 heads: 43, 27, 20; 48 heads: 46,
+// 52, 54.  bf16 heads of 128 channels, 1 and 2: 32 heads 39 and 28 us, 48 heads 41 and 52.)  Two of the small blocks of bf16 heads up to 64 channels run as fast side
+// by side (dq, 48 heads of 64 channels, 1, 2, 4: 32, 27, 43 us; 80 heads: 42, 42, 69), three in the forward pass (96 heads, 1 and 2: 22 and 19 us; 128 heads: 24 and 26), and causal
+// blocks, whose keys differ, even out when there are more.
+static int ra_wk(int32_t dtype, int d, bool dma, bool causal, int64_t pairs, int rows, bool forward = false) {
+    const int dp = ra_dp(d, dma), most = ra_most_of(dtype, dp), two = dtype == LPM_BF16 && dp <= 64 ? (forward ? 768 : 512) : causal ? 512 : 256;
+    auto blocks = [&](int wk) { return pairs * ((rows + 128 / wk - 1) / (128 / wk)); };
+    for (int wk = most; wk > 1; wk /= 2)
+        if (blocks(wk) == blocks(1) || blocks(wk) <= (wk == 2 ? two : 256)) return wk;
+    return 1;
 }
+static int ra_bm(const lpm_attn_geom& g, int32_t dtype, bool dma) { return 128 / ra_wk(dtype, g.d, dma, g.causal != 0, (int64_t)g.m * g.heads, g.pq); }
 // lines of sums by distance that a head and sample's blocks of queries leave
 static int ra_lines(const lpm_attn_geom& g, int32_t dtype, bool dma) {
-    const int bm = ra_bm(dtype, g.d, dma, (int64_t)g.m * g.heads, g.pq);
+    const int bm = ra_bm(g, dtype, dma);
     return (g.pq + bm - 1) / bm * RA_WAVES;
 }
 // The forward pass's blocks: rows folded over the heads that share keys where these fit two operands of 32 rows, and the keys over several blocks where they
 // are long and the blocks do not fill the card.
-struct RaForward { bool fold; int bm, splits; };
+struct RaForward { bool fold; int rows, splits; int64_t pairs; };
 static RaForward ra_plan(const lpm_attn_geom& g, int32_t dtype) {
     RaForward f{};
     const int share = g.heads / g.kv_heads;
     f.fold = share > 1 && g.pq <= 32 && share * g.pq <= 64 && share * ra_lut(g.reach) <= 8192;
-    const int rows = f.fold ? share * g.pq : g.pq;
-    const int64_t pairs = (int64_t)g.m * (f.fold ? g.kv_heads : g.heads);
-    f.bm = ra_bm(dtype, g.d, false, pairs, rows);
-    const int64_t blocks = std::max<int64_t>(1, pairs * ((rows + f.bm - 1) / f.bm));
+    f.rows = f.fold ? share * g.pq : g.pq;
+    f.pairs = (int64_t)g.m * (f.fold ? g.kv_heads : g.heads);
+    const int bm = 128 / ra_wk(dtype, g.d, false, g.causal != 0, f.pairs, f.rows, true);      // (what a call's pointers decide is not known here)
+    const int64_t blocks = std::max<int64_t>(1, f.pairs * ((f.rows + bm - 1) / bm));
     f.splits = blocks >= 512 ? 1 : (int)std::min<int64_t>({std::max(1, g.pk / 512), (1024 + blocks - 1) / blocks, RA_MAX_SPLITS});
     return f;
 }
@@ -1195,12 +1203,14 @@ static bool ra_dma(int32_t dtype, int d, const void* p, int64_t ldp, const void*
     return d % (16 / es) == 0 && ((uintptr_t)p | (uintptr_t)q | (uintptr_t)(ldp * es) | (uintptr_t)(ldq * es)) % 4 == 0;
 }
 // f<T, padded channels, wavefronts that share rows, DMA>
-#define LPM_RA_WIDE(f_, T_, DP_, shared_, dma_) ((shared_) ? f_<T_, DP_, ra_wide<T_, DP_>(), dma_>(a, st) : f_<T_, DP_, 1, dma_>(a, st))
-#define LPM_RA_CHANNELS(f_, T_, shared_, dma_)                                                                                                     \
-    (!(dma_) ? (a.d <= 64 ? LPM_RA_WIDE(f_, T_, 64, shared_, false) : LPM_RA_WIDE(f_, T_, 128, shared_, false))                                     \
-     : a.d <= 32 ? LPM_RA_WIDE(f_, T_, 32, shared_, true) : a.d <= 64 ? LPM_RA_WIDE(f_, T_, 64, shared_, true)                                      \
-     : a.d <= 96 ? LPM_RA_WIDE(f_, T_, 96, shared_, true) : LPM_RA_WIDE(f_, T_, 128, shared_, true))
-#define LPM_RA(f_, dtype_, shared_, dma_) ((dtype_) == LPM_BF16 ? LPM_RA_CHANNELS(f_, bf16_t, shared_, dma_) : LPM_RA_CHANNELS(f_, float, shared_, dma_))
+#define LPM_RA_WIDE(f_, T_, DP_, wk_, dma_)                                                                                                        \
+    ((wk_) == 4 ? f_<T_, DP_, ra_most<T_, DP_>(), dma_>(a, st) : (wk_) == 2 ? f_<T_, DP_, (ra_most<T_, DP_>() > 1 ? 2 : 1), dma_>(a, st)            \
+     : f_<T_, DP_, 1, dma_>(a, st))
+#define LPM_RA_CHANNELS(f_, T_, wk_, dma_)                                                                                                     \
+    (!(dma_) ? (a.d <= 64 ? LPM_RA_WIDE(f_, T_, 64, wk_, false) : LPM_RA_WIDE(f_, T_, 128, wk_, false))                                     \
+     : a.d <= 32 ? LPM_RA_WIDE(f_, T_, 32, wk_, true) : a.d <= 64 ? LPM_RA_WIDE(f_, T_, 64, wk_, true)                                      \
+     : a.d <= 96 ? LPM_RA_WIDE(f_, T_, 96, wk_, true) : LPM_RA_WIDE(f_, T_, 128, wk_, true))
+#define LPM_RA(f_, dtype_, wk_, dma_) ((dtype_) == LPM_BF16 ? LPM_RA_CHANNELS(f_, bf16_t, wk_, dma_) : LPM_RA_CHANNELS(f_, float, wk_, dma_))
 
 }  // namespace lpm
 
@@ -1289,7 +1299,7 @@ extern "C" int32_t lpm_attn_forward(const lpm_attn_geom* geom, int32_t dtype, co
     a.part_ml = (float*)((char*)ws + ra_layout(g, dtype).part_ml);
     hipStream_t st = (hipStream_t)stream;
     const bool dma = ra_dma(dtype, g.d, k, g.ldk, v, g.ldv);
-    LPM_HIP(LPM_RA(ra_forward, dtype, plan.bm < 128, dma));
+    LPM_HIP(LPM_RA(ra_forward, dtype, ra_wk(dtype, g.d, dma, a.causal, plan.pairs, plan.rows, true), dma));
     if (a.splits > 1) {
         const dim3 grid((unsigned)(((int64_t)g.m * g.heads * g.pq + RA_WAVES - 1) / RA_WAVES));
         if (dtype == LPM_BF16) hipLaunchKernelGGL(relattn_join<bf16_t>, grid, dim3(RA_THREADS), 0, st, a);
@@ -1320,8 +1330,8 @@ extern "C" int32_t lpm_attn_backward(const lpm_attn_geom* geom, int32_t dtype, c
     a.diag = dtable ? (float*)((char*)ws + o.diag) : nullptr;
     hipStream_t st = (hipStream_t)stream;
     const bool dma_k = ra_dma(dtype, g.d, k, g.ldk, v, g.ldv), dma_q = ra_dma(dtype, g.d, q, g.ldq, dy, g.ldy);
-    if (queries) LPM_HIP(LPM_RA(ra_backward_q, dtype, ra_bm(dtype, g.d, dma_k, (int64_t)g.m * g.heads, g.pq) < 128, dma_k));
-    if (keys) LPM_HIP(LPM_RA(ra_backward_kv, dtype, ra_bm(dtype, g.d, dma_q, (int64_t)g.m * g.kv_heads, g.pk) < 128, dma_q));
+    if (queries) LPM_HIP(LPM_RA(ra_backward_q, dtype, ra_wk(dtype, g.d, dma_k, a.causal, (int64_t)g.m * g.heads, g.pq), dma_k));
+    if (keys) LPM_HIP(LPM_RA(ra_backward_kv, dtype, ra_wk(dtype, g.d, dma_q, a.causal, (int64_t)g.m * g.kv_heads, g.pk), dma_q));
     if (dtable) {
         const int nd = 2 * g.reach + 1;
         float* shares = (float*)((char*)ws + o.shares);
