@@ -467,8 +467,8 @@ int32_t lpm_attn_forward(const lpm_attn_geom* g, int32_t dtype, const void* q, c
                          const int32_t* q_start, const int32_t* map, const float* table, void* y, void* stats, void* ws, void* stream);
 
 /* dq, dk, dv (laid out and spaced like q, k, v; written, keys behind key_len with zeros) and dtable (float, (+)=: accumulate = 0 overwrites, 1 adds;
- * NULL: not wanted) from dy (spaced like y) and what the forward pass read and left.  The order of every sum depends on the sizes and key_len
- * alone.  Errors: as lpm_attn_forward. */
+ * NULL: not wanted) from dy (spaced like y) and what the forward pass read and left.  The order of every sum depends on the arguments alone: the
+ * same call gives the same bits.  Errors: as lpm_attn_forward. */
 int32_t lpm_attn_backward(const lpm_attn_geom* g, int32_t dtype, const void* q, const void* k, const void* v, const void* y, const void* stats,
                           const void* dy, const int32_t* key_len, const int32_t* q_start, const int32_t* map, const float* table, void* dq,
                           void* dk, void* dv, float* dtable, int32_t accumulate, void* ws, void* stream);

