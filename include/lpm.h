@@ -444,8 +444,8 @@ int32_t lpm_norm_backward(int64_t rows, int32_t channels, int32_t dtype, const v
  *            (0: dense).  Query head h reads key and value head h / (heads / kv_heads).  A packed tensor queries | keys | values, as
  *            LPM_ATTN takes it, is three pointers into it and ldq = ldk = ldv = 3 * heads * d.  q, k, v and their gradients need the alignment
  *            of an element only.
- *   key_len  int32 [m], keys of a sample (clamped to 0 .. pk), NULL: pk.  Keys and values behind it are not read.  Values of keys that causal alone
- *            hides from some queries have to be finite.
+ *   key_len  int32 [m], keys of a sample (clamped to 0 .. pk), NULL: pk.  Keys and values behind it are not read.  Keys and values that causal alone
+ *            hides from some queries have to be finite: they are multiplied with zero.
  *   q_start  int32 [m], position of a sample's query 0 among its keys: 0 in self-attention, key_len - pq where the queries are the youngest
  *            positions of a cache; NULL: 0
  *   map      int32 [2 * reach + 1], the bucket (clamped to 0 .. n_buckets - 1) of every distance key - query from -reach to reach; distances beyond
