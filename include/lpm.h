@@ -452,6 +452,7 @@ int32_t lpm_norm_backward(int64_t rows, int32_t channels, int32_t dtype, const v
  *            have the bucket of the end.  lpm_relbias_buckets makes the usual one.
  *   table    float [heads][n_buckets]; n_buckets = 0, map = table = NULL: no bias
  *   scale    1e-30 .. 1e30; 0: 1 / sqrt(d)
+ * Results (y; dq, dk, dv, dtable) share no memory with operands.
  * Limits: d 8 .. 128, heads up to 65535, reach up to 2048, n_buckets up to 65536, pq and pk 0 .. 2^28, positions up to 2^23 elements apart. */
 typedef struct lpm_attn_geom {
     int32_t m, heads, kv_heads, pq, pk, d, causal, n_buckets, reach, ldq, ldk, ldv, ldy;

@@ -57,7 +57,7 @@ template <typename T, int DP, int WK_, bool DMA_, int OCC, bool SMALL = false> s
     static constexpr bool DMA = DMA_;
     static constexpr int EPC = Mm<T>::EPC, CHUNKS = DP / EPC, KS = DP / (2 * EPC), ES = (int)sizeof(T);
     static constexpr int BM = 128 / WK;
-    static constexpr int BN = WK > 1 ? 32 * WK : ES == 2 && !SMALL ? 64 : 32;      // rows of a staged tile
+    static constexpr int BN = WK > 1 ? 32 * WK : ES == 2 && !(SMALL && 32 * CHUNKS % RA_THREADS == 0) ? 64 : 32;      // rows of a staged tile, whole chunks of every thread
     static constexpr int SUB = BN / (32 * WK);                // 32-row pieces of it that a wavefront takes
     static constexpr int ROW = DP * ES;                       // bytes
     static constexpr int TILE = BN * ROW;
@@ -70,6 +70,7 @@ template <typename T, int DP, int WK_, bool DMA_, int OCC, bool SMALL = false> s
     static constexpr int DIAGONALS = RA_WAVES * 63 * RA_DIAG_PITCH * 4;
     static constexpr int AREAS = ES == 2 ? 2 * STAGE : LDS, LDS_Q = AREAS + DIAGONALS > LDS ? AREAS + DIAGONALS : LDS;
     static constexpr int PER = BN * CHUNKS / RA_THREADS;      // chunks of a tile a thread brings
+    static_assert(PER * RA_THREADS == BN * CHUNKS, "every chunk of a tile is brought by one thread");
     static constexpr int DT = DP / 32;                        // 32-channel pieces of a head
     static constexpr int AHEAD = DMA ? 6 : 2;                 // operands of a product on their way (8192 keys, dk and dv, 6 against 4: 847 -> 819 us)
     static constexpr int NU = 16 / EPC;                       // operands of a column of 32 probabilities
@@ -1186,6 +1187,7 @@ template <typename K> static hipError_t ra_launch(K kernel, DeviceSet& done, int
 template <typename T, int DP, int WK, bool DMA> static hipError_t ra_forward(const AttnArgs& a, hipStream_t st) {
     typedef RaFwd<T, DP, WK, DMA> R;
     static DeviceSet done;
+    static_assert(WK == 1 || 128 / WK / 32 * WK * R::DT * 4096 <= R::LDS, "the sums of wavefronts that share rows fit over the tiles");
     const int share = a.H / a.G, rows = a.fold ? share * a.pq : a.pq;
     return ra_launch(relattn_fwd<T, DP, WK, DMA>, done, (int64_t)a.m * (a.fold ? a.G : a.H) * ((rows + R::BM - 1) / R::BM) * a.splits,
                      R::LDS + 16 + (size_t)(a.fold ? share : 1) * ra_lut(a.reach) * 4, a, st);
@@ -1201,6 +1203,7 @@ template <typename T, int DP, int WK, bool DMA> static hipError_t ra_backward_q(
 template <typename T, int DP, int WK, bool DMA> static hipError_t ra_backward_kv(const AttnArgs& a, hipStream_t st) {
     typedef RaBwdKv<T, DP, WK, DMA> R;
     static DeviceSet done;
+    static_assert(WK == 1 || 128 / WK / 32 * WK * R::DT * 4096 <= R::LDS, "the sums of wavefronts that share rows fit over the tiles");
     return ra_launch(relattn_bwd_kv<T, DP, WK, DMA>, done, (int64_t)a.m * a.G * ((a.pk + R::BM - 1) / R::BM), R::LDS + (8 * R::BN + 4 + (size_t)ra_lut(a.reach)) * 4, a, st);
 }
 // Tiles straight to LDS: channels in whole chunks, every row of both operands on a whole dword

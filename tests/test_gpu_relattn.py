@@ -184,6 +184,7 @@ MORE = [
     A(2, 2, 2, 1, 4097, 128, causal=1, starts=[4096, 2500], lens=[4097, 2501], reach=2048, nb=64),
     A(1, 2, 2, 700, 700, 64, causal=1, packed=True, reach=2048, nb=5),
     A(1, 1, 1, 1500, 1500, 64, reach=128, nb=32),
+    A(130, 1, 1, 70, 1100, 72, nb=4, reach=30, lens=[1100, 600, 0, 513, 1] * 26),      # no rows shared, keys over two blocks
 ]
 
 
@@ -198,6 +199,16 @@ def test_attention(lpm, name, c):
 def test_larger_attention(lpm, name, c):
     check(lpm, c, name)
     check(lpm, c, name, train=False, seed=1)
+
+
+# as many blocks as two wavefronts share rows in, or none share any; heads that come straight from memory (16, 40, 72, 96, 128) and by way of registers
+@pytest.mark.parametrize("d", [16, 33, 40, 72, 96, 121, 128])
+@pytest.mark.parametrize("m,causal", [(50, 0), (50, 1), (200, 0), (200, 1)])
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+def test_many_blocks(lpm, name, m, causal, d):
+    r = np.random.default_rng(m + d)
+    c = A(m, 2, 2, 100, 70, d, causal=causal, nb=3, reach=11, lens=[int(x) for x in r.integers(0, 71, m)], starts=[int(x) for x in r.integers(-40, 60, m)])
+    check(lpm, c, name)
 
 
 @pytest.mark.parametrize("name", ["bf16", "f32"])
