@@ -54,6 +54,22 @@ def kept8(x):
     return q, ex, v
 
 
+def kept8_of_many(x):
+    """The same for many finite rows at once."""
+    rows, ch = x.shape
+    nb = -(-ch // 32)
+    t = np.zeros((rows, nb * 32))
+    t[:, :ch] = x
+    t = t.reshape(rows, nb, 32)
+    top = np.abs(t).max(2, keepdims=True)
+    k = np.maximum(np.frexp(top)[1] - 7, -126)          # top < 2^(k + 7): k, or the next one
+    k += top > 127 * 2.0 ** k
+    k[top == 0] = -126
+    q = np.rint(t / 2.0 ** k)
+    flat = lambda a: a.reshape(rows, nb * 32)[:, :ch]      # noqa: E731
+    return flat(q).astype(np.int8), (k[:, :, 0] + 127).astype(np.uint8), flat(q * 2.0 ** k)
+
+
 def _rows(seed, rows, ch, offset=0.0):
     r = np.random.default_rng(seed)
     x = r.standard_normal((rows, ch)) * (0.5 + r.random((rows, 1))) + 0.3 * r.standard_normal((rows, 1)) + offset
@@ -91,7 +107,7 @@ def check_norm(lpm, name, rows, ch, keep8=False, affine=True, dx_acc=False, acc=
     np.testing.assert_allclose(_np(stats).reshape(rows, 2)[:, :1], mu, rtol=0, atol=(100 * U * big).max())
     np.testing.assert_allclose(_np(stats).reshape(rows, 2)[:, 1:], rs, rtol=200 * U * (1 + (rs * big).max()))
     if keep8:
-        q, ex, X = kept8(X)
+        q, ex, X = kept8(X) if rows < 600 else kept8_of_many(X)
         n = (rows * ch + 255) // 256 * 256
         got = kept.cpu().numpy()
         assert (got[:rows * ch].view(np.int8) == q.ravel()).all() and (got[n:n + ex.size] == ex.ravel()).all()
@@ -127,6 +143,21 @@ def test_many_rows(lpm):
     """More rows than all blocks take in one turn, forward and backward."""
     check_norm(lpm, "bf16", 40000, 24)
     check_norm(lpm, "f32", 9000, 520)
+
+
+# more rows than all blocks take in one turn, forward (2048 blocks of 256 threads' rows, 64 down to one) and backward (512), for every way to share a row
+@pytest.mark.parametrize("rows,ch", [(140000, 8), (66000, 40), (33000, 100), (17000, 130), (9000, 257), (9000, 515), (9000, 1030), (2100, 2056), (2100, 4099), (2060, 8200)])
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+def test_rows_of_several_turns(lpm, name, rows, ch):
+    check_norm(lpm, name, rows, ch, keep8=(name == "bf16") == (ch % 2 == 0), dx_acc=ch % 3 == 0)
+
+
+def test_checkpoint_of_many_rows_is_the_definition():
+    r = np.random.default_rng(3)
+    x = r.standard_normal((40, 70)) * 2.0 ** r.integers(-130, 100, (40, 1))
+    x[3], x[4, :32], x[5, 5] = 0, 127 * 2.0 ** -9, 2.0 ** 90
+    for a, b in zip(kept8(x), kept8_of_many(x)):
+        assert (a == b).all()
 
 
 def test_rows_far_from_zero(lpm):
