@@ -211,6 +211,16 @@ def test_many_blocks(lpm, name, m, causal, d):
     check(lpm, c, name)
 
 
+# few queries of heads that share keys, as rows of one block: up to one operand of 32 rows, and two
+@pytest.mark.parametrize("m,heads,pq,pk", [(300, 4, 1, 60), (150, 4, 12, 90), (40, 8, 8, 90), (300, 2, 31, 40), (9, 4, 3, 1300)])
+@pytest.mark.parametrize("d", [16, 57, 64, 128])
+@pytest.mark.parametrize("name", ["bf16", "f32"])
+def test_many_blocks_of_shared_keys(lpm, name, d, m, heads, pq, pk):
+    r = np.random.default_rng(m + d)
+    lens = r.integers(0, pk + 1, m)
+    check(lpm, A(m, heads, 1, pq, pk, d, causal=1, nb=5, reach=20, lens=[int(x) for x in lens], starts=[int(x) - pq for x in lens]), name)
+
+
 @pytest.mark.parametrize("name", ["bf16", "f32"])
 def test_masks_and_values_in_masked_places(lpm, name):
     """A table of -infinity and of the lowest number in some buckets, rows of nothing else, and NaN and infinities in keys and values behind a
