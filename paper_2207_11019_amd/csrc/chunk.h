@@ -19,6 +19,20 @@ __device__ __forceinline__ void st_chunk(bf16_t* p, const float (&v)[8]) {
     const uint32_t w[4] = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
     __builtin_memcpy(p, w, 16);
 }
+// ... past the caches
+__device__ __forceinline__ void st_chunk_past(float* p, const float (&v)[8]) {
+    typedef float f4 __attribute__((ext_vector_type(4)));
+    typedef f4 at_element __attribute__((aligned(4)));
+    const f4 a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
+    __builtin_nontemporal_store(a, reinterpret_cast<at_element*>(p));
+    __builtin_nontemporal_store(b, reinterpret_cast<at_element*>(p + 4));
+}
+__device__ __forceinline__ void st_chunk_past(bf16_t* p, const float (&v)[8]) {
+    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    typedef u4 at_element __attribute__((aligned(2)));
+    const u4 w = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    __builtin_nontemporal_store(w, reinterpret_cast<at_element*>(p));
+}
 // ... the first n of them (n may be negative or more than eight)
 template <typename T> __device__ __forceinline__ void st_chunk(T* p, int n, const float (&v)[8]) {
     if (n >= 8) { st_chunk(p, v); return; }

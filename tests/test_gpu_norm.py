@@ -242,6 +242,21 @@ def test_checkpoint_of_many_rows(lpm):
         np.testing.assert_array_equal(_np(back), kept8(_np(xt))[2])
 
 
+@pytest.mark.parametrize("name,rows,ch", [("bf16", 70001, 999), ("f32", 40001, 1003), ("bf16", 140000, 512)])
+def test_checkpoint_larger_than_half_of_the_cache(lpm, name, rows, ch):
+    """Values that go past the caches: the definition's, odd channels and whole chunks."""
+    import torch
+    dt = lpm.BF16 if name == "bf16" else lpm.F32
+    xt = _torch(_rows(ch, rows, ch), name)
+    kept, back = _bytes(lpm.lpm_ckpt8_bytes(rows, ch)), torch.full((rows * ch + 8,), 3.0).to(xt.dtype).cuda()
+    lpm.lpm_ckpt8_pack(rows, ch, dt, xt.cuda(), kept)
+    lpm.lpm_ckpt8_unpack(rows, ch, dt, kept, back)
+    torch.cuda.synchronize()
+    got = _np(back)
+    assert (got[rows * ch:] == 3).all()
+    np.testing.assert_array_equal(got[:rows * ch].reshape(rows, ch), kept8_of_many(_np(xt))[2])
+
+
 # (rows of positions, image sizes) x channels: a projection, odd channels, a filter with padding
 @pytest.mark.parametrize("g", [dict(m=300, h=1, w=1, cin=64, cout=96, kh=1, kw=1, stride=1, pad=0), dict(m=50, h=1, w=1, cin=37, cout=10, kh=1, kw=1, stride=1, pad=0),
                                dict(m=2, h=9, w=7, cin=40, cout=24, kh=3, kw=3, stride=1, pad=1)], ids=lambda g: "%dx%d_%d_%d" % (g["m"], g["h"], g["cin"], g["cout"]))

@@ -18,7 +18,7 @@ def lanes(tmp_path_factory):
 
 RUNS = [
     # order of wavefronts and blocks (1: descending); file; selection
-    (1, "test_gpu_norm.py", "not graph and not many_rows and not turns and not 16383 and not 8200 and not 4099 and not 2500"),
+    (1, "test_gpu_norm.py", "not graph and not many_rows and not turns and not larger and not 16383 and not 8200 and not 4099 and not 2500"),
     (0, "test_gpu_norm.py", "channels and (257 or 65 or 2056) or checkpoint and 100"),
     (1, "test_gpu_relattn.py", "not larger and not graph and not many"),
     (0, "test_gpu_relattn.py", "test_attention and (m2_h4 or d96 or d9_)"),
